@@ -234,6 +234,68 @@ tkv_status tkv_attend_and_score_chunk(tkv_cache* c, int32_t layer, const void* q
 tkv_status tkv_decode_step(tkv_cache* c, const void* k_all, const void* v_all, const void* q_all, void* out_all,
                            void* hip_stream);
 
+/* ---- drafted trees (speculative decoding) ----------------------------------------------------------
+ * A tree of n_tree drafted tokens hangs on the committed context: node i's parent is a node before it (parents[b][i] < i), or -1 for
+ * the context's end.  A parent outside -1 .. i-1 marks a node that is not there (a batch padded to one tree size), and with it the
+ * nodes below it.  One step of a model that verifies drafts:
+ *   for every layer: tkv_append(layer, k, v, n_tree) with the nodes' rows, then tkv_attend_tree(layer, q, parents, n_tree, out);
+ *   the model's probabilities at the nodes; tkv_verify_tree; tkv_accept_tree with the path it found (or both: tkv_commit_tree).
+ * Not with TKV_PREFETCH_STREAM, and not with the redundancy-penalised scorers (EINVAL; tkv_verify_tree does not mind). */
+#define TKV_TREE_MAX 128
+
+/* Eq. 2-3 for the nodes of a tree whose rows are the layer's last n_tree positions: q device [batch, n_tree, n_q_heads, head_dim]
+ * kv_dtype, parents device int32 [batch, n_tree], out device, q's shape, in out_dtype.  A node attends to every live position before
+ * the tree, to its ancestors and to itself.  The output of a node that is not there is zero, and its rows are nobody's, whatever they
+ * hold; the rows and queries of the others must be finite.  Adds nothing to the scores: whether a node stays is not known yet; the
+ * softmax statistics that tkv_accept_tree needs stay in the handle until the cache's length changes.  T1 placement is bit-invisible
+ * (Prop. 1); outputs agree with those of single-token steps to binary32 rounding, with 16-bit rows to 1e-6 (two 16-bit terms per
+ * weight).  The first call, and the first with more than 16, 32 or 64 nodes, allocates scratch (not while its stream is captured).
+ * EINVAL beyond TKV_TREE_MAX nodes; ESTATE unless the n_tree positions are in the cache of every sequence and were appended after the
+ * last tkv_migrate. */
+tkv_status tkv_attend_tree(tkv_cache* c, int32_t layer, const void* q, const int32_t* parents, int32_t n_tree, void* out, void* hip_stream);
+
+/* Speculative sampling over a tree, from given random numbers.  All pointers are device pointers. */
+typedef struct {
+  const int32_t* parents;              /* [batch, n_tree]; node 0 is the root, the last token that is certain */
+  const int32_t* tokens;               /* [batch, n_tree]; the root's is not read.  One outside 0 .. vocab-1 is not taken */
+  const void* p;                       /* [batch, n_tree] rows: the target's probabilities after each node */
+  const void* q;                       /* [batch, n_tree] rows: the draft's, which a node's children were drawn from one by one; or NULL:
+                                          children are different tokens chosen by rank */
+  int64_t p_stride, q_stride;          /* elements from row to row */
+  const float* u_accept;               /* [batch, n_tree] uniform in [0, 1): node i's test */
+  const float* u_draw;                 /* [batch] uniform in [0, 1): the next token */
+  int32_t* path;                       /* out [batch, n_tree]: the nodes taken, from the root down, then -1 */
+  int32_t* n_path;                     /* out [batch]: how many (at least 1) */
+  int32_t* next;                       /* out [batch]: the token behind the last node taken */
+  int32_t n_tree, vocab, prob_dtype;   /* prob_dtype: tkv_dtype of p and q */
+} tkv_tree_walk;
+
+/* From the root, with t = p[root] and S = 1: the children x of the current node, in order of their index, are tested one by one.
+ *   q given:  taken if u * S * q[x] < t[x]; else t = max(t - S * q, 0) and S = sum(t).
+ *   q NULL:   taken if u * S < t[x]; else S = S - t[x] and t[x] = 0.
+ * A child that is taken becomes the current node, with its own p and S = 1.  A residual without anything in it (p and q are rounded) is
+ * not made: t stays.  When no child is left, next is the smallest token whose running sum of t exceeds u_draw times the whole.
+ * Residuals and sums are 64-bit.  With q (whose children are independent draws from it) or ranked children every path's tokens are
+ * distributed as the target's own.  Probabilities must be finite and not negative.  Needs no layer's state, and any
+ * prefetch mode and scorer; the first call allocates its scratch. */
+tkv_status tkv_verify_tree(tkv_cache* c, const tkv_tree_walk* w, void* hip_stream);
+
+/* Keeps some of the last n_tree positions: path device int32 [batch, n_path], ascending node indices, ended by -1 (or by n_path).
+ * With base = length - n_tree, sequence b's node path[b][j] becomes position base + j, in every layer (its slot changes hands, no row
+ * moves); the other nodes' slots are free again.  The cache's length becomes base + the longest path's; in sequences that keep less,
+ * the positions beyond their own path are evicted (T3).  n_path = 0 (path NULL) takes the last n_tree positions back.
+ * *n_kept (host; may be NULL): the longest path's nodes.
+ * Scores: q_all device [n_layers, batch, n_tree, n_q_heads, head_dim], the queries that every layer's tkv_attend_tree had: each kept
+ * node's weights are added to the scores of the positions it attended to, as its single-token step would have (Eq. 1, or times the
+ * value rows' norms).  q_all NULL: no score changes.  A kept position keeps what was in its score.
+ * Reads the counts back (one short synchronisation), like tkv_migrate.  EINVAL for a path that is not ascending within the tree;
+ * ESTATE if layers differ in length, a tier plan is pending, the positions were there before the last tkv_migrate, or (q_all) a layer
+ * has not been attended with this tree; nothing has changed then. */
+tkv_status tkv_accept_tree(tkv_cache* c, int32_t n_tree, const int32_t* path, int32_t n_path, const void* q_all, int32_t* n_kept, void* hip_stream);
+
+/* tkv_verify_tree, then tkv_accept_tree with the path it found (w->path; the host does not see it in between). */
+tkv_status tkv_commit_tree(tkv_cache* c, const tkv_tree_walk* w, const void* q_all, int32_t* n_kept, void* hip_stream);
+
 /* Sec. 3.3 / Algorithm 1 "tier management", device only: ranks the candidates of every sequence by
  * (already evicted first, score bits, position) and writes the pending tier array; no KV row moves.
  * ESTATE if layers differ in length; EINVAL if the policy does not sum to 10^6. */

@@ -59,6 +59,12 @@ class tkv_stats(C.Structure):
     ]
 
 
+class tkv_tree_walk(C.Structure):
+    _fields_ = [("parents", C.c_void_p), ("tokens", C.c_void_p), ("p", C.c_void_p), ("q", C.c_void_p), ("p_stride", C.c_int64), ("q_stride", C.c_int64),
+                ("u_accept", C.c_void_p), ("u_draw", C.c_void_p), ("path", C.c_void_p), ("n_path", C.c_void_p), ("next", C.c_void_p),
+                ("n_tree", C.c_int32), ("vocab", C.c_int32), ("prob_dtype", C.c_int32)]
+
+
 # every symbol include/tkv.h declares: name -> (restype, argtypes)
 _VP, _I32 = C.c_void_p, C.c_int32
 SYMBOLS = {
@@ -69,6 +75,10 @@ SYMBOLS = {
     "tkv_attend_and_score_noalloc": (C.c_int, [_VP, _I32, _VP, _VP, _VP]),
     "tkv_attend_and_score_chunk": (C.c_int, [_VP, _I32, _VP, _VP, _I32, _VP]),
     "tkv_decode_step": (C.c_int, [_VP, _VP, _VP, _VP, _VP, _VP]),
+    "tkv_attend_tree": (C.c_int, [_VP, _I32, _VP, _VP, _I32, _VP, _VP]),
+    "tkv_verify_tree": (C.c_int, [_VP, C.POINTER(tkv_tree_walk), _VP]),
+    "tkv_accept_tree": (C.c_int, [_VP, _I32, _VP, _I32, _VP, C.POINTER(_I32), _VP]),
+    "tkv_commit_tree": (C.c_int, [_VP, C.POINTER(tkv_tree_walk), _VP, C.POINTER(_I32), _VP]),
     "tkv_set_profile": (C.c_int, [_VP, _I32]),
     "tkv_classify": (C.c_int, [_VP, C.POINTER(tkv_policy), _VP]),
     "tkv_migrate": (C.c_int, [_VP, _VP]),
@@ -285,6 +295,89 @@ class TieredKV:
                                              self._dev_tensor(out_all, (L, B, Hq, D), self.out_torch_dtype),
                                              self._stream(stream)))
         return out_all
+
+    # -- drafted trees ---------------------------------------------------------------------------------
+    def _int_tensor(self, t, shape):
+        assert t.device == self.device and t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == tuple(shape), (t.device, t.dtype, t.shape, shape)
+        return t.data_ptr()
+
+    def _own_stream(self, stream):
+        return _current_raw_stream(self.device.index) if stream is None else stream.cuda_stream
+
+    def attend_tree(self, layer, q, parents, out=None, stream=None):
+        """Attention of a drafted tree whose rows are the layer's last positions: q [B, n, Hq, D], parents int32 [B, n]."""
+        L, B, Hq, Hkv, D = self.shape
+        n = int(q.shape[1])
+        if out is None:
+            out = torch.empty((B, n, Hq, D), dtype=self.out_torch_dtype, device=self.device)
+        self._call_stream = stream       # the first tree of a size allocates its scratch
+        try:
+            self._check(self.lib.tkv_attend_tree(self._h, layer, self._dev_tensor(q, (B, n, Hq, D)), self._int_tensor(parents, (B, n)), n,
+                                                 self._dev_tensor(out, (B, n, Hq, D), self.out_torch_dtype), self._own_stream(stream)))
+        finally:
+            self._call_stream = None
+        return out
+
+    def _walk(self, parents, tokens, p, u_accept, u_draw, q):
+        B, n, vocab = self.shape[1], int(parents.shape[1]), int(p.shape[2])
+        kinds = {torch.float32: TKV_F32, torch.bfloat16: TKV_BF16, torch.float16: TKV_F16}
+        w = tkv_tree_walk()
+        w.parents, w.tokens = self._int_tensor(parents, (B, n)), self._int_tensor(tokens, (B, n))
+        for name, t in (("p", p), ("q", q)):
+            if t is None:
+                continue
+            assert t.device == self.device and t.dtype == p.dtype and t.dtype in kinds and tuple(t.shape) == (B, n, vocab), (t.device, t.dtype, t.shape, (B, n, vocab))
+            rows = t.stride(1) if n > 1 else t.stride(0) if B > 1 else vocab
+            assert (vocab == 1 or t.stride(2) == 1) and rows >= vocab and (B == 1 or t.stride(0) == n * rows), f"rows of {name} must lie one after another, {t.stride()}"
+            setattr(w, name, t.data_ptr())
+            setattr(w, name + "_stride", rows)
+        for t, shape in ((u_accept, (B, n)), (u_draw, (B,))):
+            assert t.device == self.device and t.dtype == torch.float32 and t.is_contiguous() and tuple(t.shape) == shape, (t.device, t.dtype, t.shape, shape)
+        w.u_accept, w.u_draw = u_accept.data_ptr(), u_draw.data_ptr()
+        path, n_path, token = (torch.empty(s, dtype=torch.int32, device=self.device) for s in ((B, n), (B,), (B,)))
+        w.path, w.n_path, w.next = path.data_ptr(), n_path.data_ptr(), token.data_ptr()
+        w.n_tree, w.vocab, w.prob_dtype = n, vocab, kinds[p.dtype]
+        return w, path, n_path, token
+
+    def verify_tree(self, parents, tokens, p, u_accept, u_draw, q=None, stream=None):
+        """Walks a drafted tree against the target's probabilities p [B, n, vocab] (q: the draft's, or None for children chosen by
+        rank), from random numbers u_accept [B, n] and u_draw [B].  Returns path [B, n], n_path [B] and the next token [B], int32."""
+        self._call_stream = stream
+        try:
+            with torch.cuda.stream(stream):          # (None: the current one) the outputs are written on it
+                w, path, n_path, token = self._walk(parents, tokens, p, u_accept, u_draw, q)
+            self._check(self.lib.tkv_verify_tree(self._h, C.byref(w), self._own_stream(stream)))
+        finally:
+            self._call_stream = None
+        return path, n_path, token
+
+    def accept_tree(self, n_tree, path=None, q_all=None, stream=None):
+        """Keeps the nodes path [B, m] (int32, ended by -1) of the last n_tree positions, or none of them; q_all [L, B, n_tree, Hq, D]:
+        their weights enter the scores.  Returns how many positions the longest path has."""
+        L, B, Hq, Hkv, D = self.shape
+        kept = C.c_int32(0)
+        n_path = 0 if path is None else int(path.shape[1])
+        self._call_stream = stream
+        try:
+            self._check(self.lib.tkv_accept_tree(self._h, n_tree, None if path is None else self._int_tensor(path, (B, n_path)), n_path,
+                                                 None if q_all is None else self._dev_tensor(q_all, (L, B, n_tree, Hq, D)), C.byref(kept), self._own_stream(stream)))
+        finally:
+            self._call_stream = None
+        return int(kept.value)
+
+    def commit_tree(self, parents, tokens, p, u_accept, u_draw, q=None, q_all=None, stream=None):
+        """verify_tree, then accept_tree with the path found.  Returns (kept, path, n_path, next token)."""
+        L, B, Hq, Hkv, D = self.shape
+        kept = C.c_int32(0)
+        self._call_stream = stream
+        try:
+            with torch.cuda.stream(stream):
+                w, path, n_path, token = self._walk(parents, tokens, p, u_accept, u_draw, q)
+            self._check(self.lib.tkv_commit_tree(self._h, C.byref(w), None if q_all is None else self._dev_tensor(q_all, (L, B, w.n_tree, Hq, D)),
+                                                 C.byref(kept), self._own_stream(stream)))
+        finally:
+            self._call_stream = None
+        return int(kept.value), path, n_path, token
 
     def set_profile(self, on):
         self._check(self.lib.tkv_set_profile(self._h, int(on)))

@@ -11,6 +11,9 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtkv.so")
 # (source, extra flags, object name); the attention kernels are one source compiled in seven parts that build in parallel
 UNITS = [("attn_kernels.hip", [f"-DTKV_ATTN_PART={p}"], f"attn_kernels_{p}.o") for p in range(7)]
+# ... those of drafted trees in seven more, one per row type and head_dim
+UNITS += [("tree_kernels.hip", [f"-DTKV_TREE_PART={p}"], f"tree_kernels_{p}.o") for p in range(7)]
+UNITS += [("walk_kernels.hip", [], "walk_kernels.o")]
 UNITS += [("tkv_host.hip", [], "tkv_host.o"), ("tier_kernels.hip", [], "tier_kernels.o")]
 # packed-fp32 VALU forms are switched off on purpose (the compiler would otherwise emit them from plain float code)
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -87,21 +90,19 @@ def build_host_check(verbose: bool = False) -> str:
     return HOST_CHECK
 
 
-FAKE_CHECK = os.path.join(HERE, "_build", "fake_runtime_check")
-
-
-def build_fake_check() -> str:
+def build_fake_check(name: str = "fake_runtime_check") -> str:
     """The library's objects linked with tests/native/fake_runtime_check.cpp, which takes the HIP runtime's place: the
-    host code's launches and allocations on a machine without a GPU.  Uses the objects build() leaves in _build/."""
+    host code's launches and allocations on a machine without a GPU (tree_host_check: the same for drafted trees).  Uses the
+    objects build() leaves in _build/."""
     objs = [os.path.join(HERE, "_build", n) for _, _, n in UNITS]
     if not all(os.path.exists(o) for o in objs):
         build()
-    src = os.path.join(os.path.dirname(HERE), "tests", "native", "fake_runtime_check.cpp")
+    src, exe = os.path.join(os.path.dirname(HERE), "tests", "native", f"{name}.cpp"), os.path.join(HERE, "_build", name)
     r = subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include", src, *objs,
-                        "-lpthread", "-o", FAKE_CHECK], capture_output=True, text=True)
+                        "-lpthread", "-o", exe], capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("g++ failed:\n" + r.stderr)
-    return FAKE_CHECK
+    return exe
 
 
 if __name__ == "__main__":

@@ -42,24 +42,18 @@
 #include <algorithm>
 #include <utility>
 
-#include "tkv_internal.h"
+#include "device_common.h"
 
 namespace tkv {
 
-typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
 typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) char lds_char;
 
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr int TB = TOK_PER_BLOCK;
 static_assert(TB == 64, "a tile is one list entry per lane");
 
 enum Mode : int { F_BF16 = 0, F_F32 = 1, Q_INT8 = 2, Q_INT4 = 3, F_F16 = 4 };
-// type of K, V and q as a template argument: binary32, bfloat16, binary16
-constexpr int KT_F32 = 0, KT_BF16 = 1, KT_F16 = 2;
 
 template <class F, int... I>
 __device__ __forceinline__ void static_for_impl(F&& f, std::integer_sequence<int, I...>) {
@@ -91,7 +85,6 @@ __device__ __forceinline__ u32x4 lds_rd128(uint32_t addr) {
   asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF) : "memory");
   return v;
 }
-typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
 template <int OFF>
 __device__ __forceinline__ u32x2 lds_rd64(uint32_t addr) {
   u32x2 v;
@@ -223,10 +216,6 @@ __device__ __forceinline__ float wave_sum(float x) {
 // a fraction of what a shuffle per value costs (1.4 us for 56 values per lane, 0.2 us this way).
 template <int EV, int LPRV>
 struct RowSum { static constexpr int N = EV * LPRV / 64; };
-__device__ __forceinline__ float add_swap32(float a, float b) {      // lanes 0..31: a's halves added; 32..63: b's
-  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), false, false);
-  return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
-}
 __device__ __forceinline__ float add_swap16(float a, float b) {      // even rows: a's row pair added; odd rows: b's
   const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), false, false);
   return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
@@ -267,11 +256,6 @@ __device__ __forceinline__ int row_sum_elem(int lane, int k) {
 
 __device__ __forceinline__ float bf_lo(uint32_t u) { return __builtin_bit_cast(float, u << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t u) { return __builtin_bit_cast(float, u & 0xffff0000u); }
-__device__ __forceinline__ uint16_t f32_to_bf16(float f) {
-  uint32_t u = __builtin_bit_cast(uint32_t, f);
-  u += 0x7fffu + ((u >> 16) & 1u);
-  return (uint16_t)(u >> 16);
-}
 // two code values (exact in binary16) packed as a binary16 pair
 __device__ __forceinline__ uint32_t pack_f16_pair(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(lo, hi));
@@ -281,9 +265,6 @@ __device__ __forceinline__ float f16_hi(uint32_t u) { return (float)__builtin_bi
 // two code values (exact in bf16: at most 8 significant bits) packed as a bf16 pair
 __device__ __forceinline__ uint32_t pack_bf16_pair(float lo, float hi) {
   return (__builtin_bit_cast(uint32_t, hi) & 0xffff0000u) | (__builtin_bit_cast(uint32_t, lo) >> 16);
-}
-__device__ __forceinline__ float half_of(uint32_t w, int hi) {
-  return (float)__builtin_bit_cast(_Float16, (uint16_t)(hi ? (w >> 16) : (w & 0xffffu)));
 }
 
 // Logits of one call: [sequence entry][query head][xs_stride], by list index; scaled, but of one token on the matrix cores
@@ -505,8 +486,6 @@ struct WaveLds {
   uint32_t lga; int lcap, lim;             // k_attn_step: logits [G][lcap] in LDS; the columns from lim (whole tiles: lcap, or
   float* sp; int sp_stride;                // none for a part of a pair) on go to memory, column c of head h to sp[h * sp_stride + c]
 };
-
-struct __attribute__((packed, aligned(2))) PackedU32x4 { u32x4 v; };   // 16 bytes at any 16-bit element
 
 template <int SZ>
 __device__ __forceinline__ void dma(const __amdgpu_buffer_rsrc_t& rs, char* lds, uint32_t voff, int aux) {
@@ -892,10 +871,6 @@ __device__ __forceinline__ void attn_wave(const AttnArgs& a, const WaveLds& w, i
 // operand read (16 different rows, same piece) fall on 16 different bank groups; the rotation is undone by the read
 // addresses.  K rows of a tile, its V rows and the next tile's K rows pass through the one tile buffer as in attn_wave:
 // the K rows of 16 entries are replaced by V pieces once read, half a tile of V rows by the next tile's K pieces.
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-
 template <int KT>
 __device__ __forceinline__ f32x4 mfma_16x16x32(const u32x4& x, const u32x4& y, f32x4 c) {
   if constexpr (KT == KT_BF16)
@@ -960,27 +935,6 @@ __device__ __forceinline__ void split_pair(float& p0, float& p1, uint32_t (&t)[N
       p1 -= (float)h.y;
     }
   }
-}
-
-// Code values (one byte each, or two per byte) as 16-bit floating point, sign-extended: at most 7 significant bits, so the
-// matrix cores multiply them exactly.  Two values per 32-bit word, low element first.
-template <int KT>
-__device__ __forceinline__ uint32_t pack16(float lo, float hi) {
-  if constexpr (KT == KT_BF16) return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
-  else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(lo, hi));
-}
-__device__ __forceinline__ float sbyte_f(uint32_t w, int n) { return (float)(int8_t)(w >> (8 * n)); }              // byte n of w
-__device__ __forceinline__ float snib_f(uint32_t w, int n) { return (float)((int32_t)(w << (28 - 4 * n)) >> 28); }   // nibble n of w
-// one word of int8 codes (4) -> two words; one word of int4 codes (8) -> four words
-template <int KT>
-__device__ __forceinline__ void widen_int8(uint32_t w, uint32_t& o0, uint32_t& o1) {
-  o0 = pack16<KT>(sbyte_f(w, 0), sbyte_f(w, 1));
-  o1 = pack16<KT>(sbyte_f(w, 2), sbyte_f(w, 3));
-}
-template <int KT>
-__device__ __forceinline__ u32x4 widen_int4(uint32_t w) {
-  return u32x4{pack16<KT>(snib_f(w, 0), snib_f(w, 1)), pack16<KT>(snib_f(w, 2), snib_f(w, 3)),
-               pack16<KT>(snib_f(w, 4), snib_f(w, 5)), pack16<KT>(snib_f(w, 6), snib_f(w, 7))};
 }
 
 // M: F_BF16 / F_F16 (list F; the element type is KT's) or Q_INT8 / Q_INT4 (list Q).  NCB: blocks of 16 columns, the first

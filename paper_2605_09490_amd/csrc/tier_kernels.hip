@@ -187,7 +187,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_classify(DevView v, int n, Ppm
   const int lo = v.n_prompt + v.k_sink;
   const int hi = n - v.k_window;
   if (hi <= lo) {
-    for (int i = t; i < n; i += PLAN_THREADS) tnew[i] = 0;
+    for (int i = t; i < n; i += PLAN_THREADS) tnew[i] = tier[i] == 3 ? 3 : 0;   // (a drafted node that was not kept)
     return;
   }
   const int m = hi - lo;
@@ -241,7 +241,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_classify(DevView v, int n, Ppm
   __syncthreads();
   const uint64_t th3 = sh_thr[0], th2 = sh_thr[1], th1 = sh_thr[2];
   for (int i = t; i < n; i += PLAN_THREADS) {
-    uint8_t c = 0;
+    uint8_t c = tier[i] == 3 ? 3 : 0;
     if (i >= lo && i < hi) {
       const uint64_t key = rank_key(tier[i], score[i], i);
       c = key < th3 ? 3 : key < th2 ? 2 : key < th1 ? 1 : 0;

@@ -17,6 +17,7 @@
 
 #include "../../include/tkv.h"
 #include "tkv_internal.h"
+#include "tree.h"
 
 using namespace tkv;
 
@@ -81,6 +82,17 @@ struct tkv_cache {
   int sc_stride = 0, spill_stride = 0;
   int tail_pairs = 0, tail_parts = 1;   // of a whole-pair step the last tail_pairs (layer, sequence, kv head) pairs go in tail_parts parts each
   float* xt_tail = nullptr; float* ml_tail = nullptr; float* po_tail = nullptr;   // (none: a layer's in the scratch of the single calls)
+  // drafted trees: scratch for trees of up to tree_cap nodes, and which layers have been attended with which tree since the last
+  // append or accept (their columns' statistics are in stat_tree)
+  int tree_cap = 0;
+  float* ml_tree = nullptr; float* po_tree = nullptr; float2* stat_tree = nullptr; int* here_tree = nullptr;
+  float* gain_tree = nullptr;      // kept queries' weights, gain_layers layers at a time
+  int gain_layers = 0, gain_stride = 0;
+  int* info_tree = nullptr; int* pin_info = nullptr;   // [B][2] nodes kept, slots held
+  double* walk_part = nullptr; int* walk_arrived = nullptr;
+  std::vector<int> tree_nodes, tree_len;   // per layer: nodes, and positions assigned, of the tree it was attended with (0: none)
+  int64_t gaps = 0;                // positions after the last plan that are missing in a sequence (nodes that were not kept), all sequences
+  int whole_from = 0;              // none from here on
   int S_alloc = 0, xs_stride = 0;
   int cus = 0;                     // compute units of the device
   char* static_scratch = nullptr;  // this device's copy of the library's fixed scratch array (tkv_attend_and_score_noalloc)
@@ -672,6 +684,7 @@ tkv_status tkv_create(const tkv_config* cfg, tkv_cache** out) {
   c->ev_ready.assign(L, nullptr);
   c->layer_wait.assign(L, 0);
   c->layer_enq.assign(L, 0);
+  c->tree_nodes.assign(L, 0); c->tree_len.assign(L, 0);
   // default-priority streams only
   if (hipStreamCreateWithFlags(&c->sA, hipStreamNonBlocking) != hipSuccess ||
       hipStreamCreateWithFlags(&c->sB, hipStreamNonBlocking) != hipSuccess)
@@ -778,6 +791,32 @@ static tkv_status chunk_scratch(tkv_cache* c) {
   return TKV_OK;
 }
 
+// Layers whose T1 rows may still be on their way (layer .. layer + nl - 1): WAIT orders the stream behind them, LAZY sets the bit of
+// a layer that is to read the rows' old slots.
+static tkv_status settle_rows(tkv_cache* c, int32_t layer, int nl, bool noalloc, hipStream_t st, uint64_t& old_mask) {
+  for (int li = 0; li < nl; ++li) {
+    const int l = layer + li;
+    if (!c->layer_wait[l]) continue;
+    if (c->cfg.prefetch_mode == TKV_PREFETCH_WAIT) {
+      while (!noalloc && !c->layer_enq[l] && c->jobs_next < c->jobs.size()) {
+        tkv_status ps = pump_transfers(c, 1);
+        if (ps != TKV_OK) return ps;
+      }
+      if (!c->layer_enq[l]) return fail(c, TKV_ESTATE, "tkv_attend_and_score: the transfers of layer %d have not been queued", l);
+      HIPCHK(c, hipStreamWaitEvent(st, c->ev_ready[l], 0));
+      c->layer_wait[l] = 0;
+      c->st.attend_waits++;
+    } else {
+      // a layer whose pieces are still queued on the host keeps its old slots, like one whose copies are in flight
+      hipError_t e = c->layer_enq[l] ? hipEventQuery(c->ev_ready[l]) : hipErrorNotReady;
+      if (e == hipSuccess) c->layer_wait[l] = 0;
+      else if (e == hipErrorNotReady) { old_mask |= 1ull << li; c->st.lazy_old_reads++; }
+      else return fail(c, TKV_EDEVICE, "hipEventQuery failed: %s", hipGetErrorString(e));
+    }
+  }
+  return TKV_OK;
+}
+
 // m query tokens per sequence (m = 1: a decode step's one) against one layer.  trim: entries at the end of list F that
 // the last of the m queries leaves out (later tokens of a chunk); query j of the m leaves m - 1 - j more out.  q_bs /
 // o_bs: query heads between consecutive sequences in q / out, the m queries of a sequence being Hq heads apart; last:
@@ -806,26 +845,8 @@ static tkv_status attend_one(tkv_cache* c, int32_t layer, const void* q, void* o
       c->st.attend_waits++;
     }
   } else {
-    for (int li = 0; li < nl; ++li) {
-      const int l = layer + li;
-      if (!c->layer_wait[l]) continue;
-      if (c->cfg.prefetch_mode == TKV_PREFETCH_WAIT) {
-        while (!noalloc && !c->layer_enq[l] && c->jobs_next < c->jobs.size()) {
-          tkv_status ps = pump_transfers(c, 1);
-          if (ps != TKV_OK) return ps;
-        }
-        if (!c->layer_enq[l]) return fail(c, TKV_ESTATE, "tkv_attend_and_score: the transfers of layer %d have not been queued", l);
-        HIPCHK(c, hipStreamWaitEvent(st, c->ev_ready[l], 0));
-        c->layer_wait[l] = 0;
-        c->st.attend_waits++;
-      } else {
-        // a layer whose pieces are still queued on the host keeps its old slots, like one whose copies are in flight
-        hipError_t e = c->layer_enq[l] ? hipEventQuery(c->ev_ready[l]) : hipErrorNotReady;
-        if (e == hipSuccess) c->layer_wait[l] = 0;
-        else if (e == hipErrorNotReady) { old_mask |= 1ull << li; c->st.lazy_old_reads++; }
-        else return fail(c, TKV_EDEVICE, "hipEventQuery failed: %s", hipGetErrorString(e));
-      }
-    }
+    const tkv_status rs = settle_rows(c, layer, nl, noalloc, st, old_mask);
+    if (rs != TKV_OK) return rs;
   }
   auto tiles = [](int n) { return (n + TOK_PER_BLOCK - 1) / TOK_PER_BLOCK; };
   int n_tiles = 1, n_tiles_s = 0;
@@ -980,6 +1001,8 @@ tkv_status tkv_attend_and_score_chunk(tkv_cache* c, int32_t layer, const void* q
   // the chunk's positions must be the tail of list F: appended since the last plan was applied, so still in T0
   if (n_q > c->n_assigned - c->n_at_plan)
     return fail(c, TKV_ESTATE, "tkv_attend_and_score_chunk: %d query tokens, but only %d positions were appended since the last tkv_migrate", n_q, c->n_assigned - c->n_at_plan);
+  if (n_q > c->n_assigned - c->whole_from)
+    return fail(c, TKV_ESTATE, "tkv_attend_and_score_chunk: %d query tokens, but positions below %d are missing in some sequences", n_q, c->whole_from);
   const DevView& v = c->dv;
   const size_t q_tok = (size_t)v.Hq * v.D * c->es, o_tok = (size_t)v.Hq * v.D * (c->cfg.out_dtype == TKV_F32 ? 4 : 2);
   // The chunk's tokens go in groups of as many as one launch takes.  The streamed mode, whose frame serves one launch pair at
@@ -992,6 +1015,208 @@ tkv_status tkv_attend_and_score_chunk(tkv_cache* c, int32_t layer, const void* q
     if (s != TKV_OK) return s;
   }
   return TKV_OK;
+}
+
+// ---- drafted trees -----------------------------------------------------------------------------------------
+namespace {
+// The handle's device is current while one of these calls runs, whichever was before.
+struct DeviceScope {
+  int before = -1;
+  bool ok = true;
+  explicit DeviceScope(int device) {
+    ok = hipGetDevice(&before) == hipSuccess && (before == device || hipSetDevice(device) == hipSuccess);
+    if (!ok || before == device) before = -1;
+  }
+  ~DeviceScope() { if (before >= 0) (void)hipSetDevice(before); }
+};
+#define ON_DEVICE(c) DeviceScope scope_((c)->cfg.device); if (!scope_.ok) return fail((c), TKV_EDEVICE, "hipSetDevice failed")
+
+const char* tree_refusal(const tkv_cache* c) {
+  if (c->streamed) return "not available with TKV_PREFETCH_STREAM";
+  if (c->cfg.scorer == TKV_SCORE_REDUNDANCY || c->cfg.scorer == TKV_SCORE_COMBINED)
+    return "not available with the redundancy-penalised scorers (a row's redundancy is taken against the row appended before it)";
+  return nullptr;
+}
+// splits of a pair's tiles: workgroups for all compute units, of four tiles or more
+int tree_splits(const tkv_cache* c, int n) {
+  const DevView& v = c->dv;
+  const TreeShape s = tree_shape(v.D, c->kt, n * c->G);
+  const int tr = tree_tile_rows(s), units = tree_units(c->kt, s, c->cus), per = v.B * v.Hkv * s.groups;
+  int tiles = 1;
+  for (int b = 0; b < v.B; ++b) tiles = std::max(tiles, (c->nF[b] + tr - 1) / tr + (c->nQ[b] + tr - 1) / tr);
+  return std::max(1, std::min({units / per, (tiles + 3) / 4, 64}));
+}
+// Scratch for trees of n nodes: partials for as many splits as there may be, statistics of all layers.
+tkv_status tree_scratch(tkv_cache* c, int n) {
+  if (n <= c->tree_cap) return TKV_OK;
+  const DevView& v = c->dv;
+  int cap = 16;
+  while (cap < n) cap *= 2;
+  size_t cols = 0;                                       // (pair, split, column)s
+  for (int m = 1; m <= cap; ++m) {
+    const TreeShape s = tree_shape(v.D, c->kt, m * c->G);
+    const size_t pairs = (size_t)v.B * v.Hkv, S = std::min<size_t>(64, std::max<size_t>(1, (size_t)tree_units(c->kt, s, c->cus) / (pairs * s.groups)));
+    cols = std::max(cols, S == 1 ? 0 : pairs * S * m * c->G);
+  }
+  float *ml = nullptr, *po = nullptr;
+  float2* stat = nullptr;
+  int* here = nullptr;
+  if (!dalloc(c, ml, cols * 2) || !dalloc(c, po, cols * v.D) || !dalloc(c, stat, (size_t)v.L * v.B * v.Hq * cap) || !dalloc(c, here, (size_t)v.B * cap))
+    return fail(c, TKV_ENOMEM, "tkv_attend_tree: no device memory for the scratch of %d nodes", cap);
+  c->ml_tree = ml; c->po_tree = po; c->stat_tree = stat; c->here_tree = here;
+  c->tree_cap = cap;
+  std::fill(c->tree_nodes.begin(), c->tree_nodes.end(), 0);    // (the statistics start anew)
+  return TKV_OK;
+}
+}  // namespace
+
+tkv_status tkv_attend_tree(tkv_cache* c, int32_t layer, const void* q, const int32_t* parents, int32_t n_tree, void* out, void* hip_stream) {
+  if (!c) return TKV_EINVAL;
+  if (layer < 0 || layer >= c->cfg.n_layers || !q || !out || !parents || n_tree < 1 || n_tree > TKV_TREE_MAX)
+    return fail(c, TKV_EINVAL, "tkv_attend_tree: bad argument (1 to %d nodes)", TKV_TREE_MAX);
+  if (const char* why = tree_refusal(c)) return fail(c, TKV_EINVAL, "tkv_attend_tree: %s", why);
+  if (c->len[layer] != c->n_assigned) return fail(c, TKV_ESTATE, "tkv_attend_tree: layer %d has %d tokens, %d are assigned; append first", layer, c->len[layer], c->n_assigned);
+  const int fresh = c->n_assigned - std::max(c->n_at_plan, c->whole_from);
+  if (n_tree > fresh)
+    return fail(c, TKV_ESTATE, "tkv_attend_tree: %d nodes, but only %d positions were appended since the last tkv_migrate or tkv_accept_tree that left gaps", n_tree, fresh);
+  ON_DEVICE(c);
+  tkv_status s = tree_scratch(c, n_tree);
+  if (s != TKV_OK) return s;
+  hipStream_t st = (hipStream_t)hip_stream;
+  uint64_t old_mask = 0;
+  s = settle_rows(c, layer, 1, false, st, old_mask);
+  if (s != TKV_OK) return s;
+  const DevView& v = c->dv;
+  const size_t lrows = (size_t)layer * v.B * v.Hkv;
+  TreeArgs a{};
+  a.fpK = v.fpK + lrows * v.capP * v.D * v.es; a.fpV = v.fpV + lrows * v.capP * v.D * v.es;
+  a.c2K = v.c2K + lrows * v.cap2 * v.cb; a.c2V = v.c2V + lrows * v.cap2 * v.cb;
+  a.s2K = v.s2K + lrows * v.cap2 * v.sb; a.s2V = v.s2V + lrows * v.cap2 * v.sb;
+  a.q = q; a.out = out; a.parents = parents;
+  a.f_loc = old_mask ? v.f_loc_old : v.f_loc; a.f_pos = v.f_pos; a.q_loc = v.q_loc; a.q_pos = v.q_pos;
+  a.cnt = v.cnt; a.part_ml = c->ml_tree; a.part_o = c->po_tree; a.here = c->here_tree;
+  a.B = v.B; a.Hq = v.Hq; a.Hkv = v.Hkv; a.G = c->G; a.n = n_tree; a.C = n_tree * c->G;
+  a.stat_stride = c->tree_cap * c->G; a.stat = c->stat_tree + lrows * a.stat_stride;
+  a.S = tree_splits(c, n_tree); a.groups = tree_shape(v.D, c->kt, a.C).groups;
+  a.Nmax = v.Nmax; a.capF = v.capP; a.cap2 = v.cap2; a.cb = v.cb; a.sb = v.sb; a.t2fmt = v.t2fmt; a.out_kind = c->cfg.out_dtype;
+  a.scale2 = c->softmax_scale * 1.4426950408889634f;
+  if (v.B <= ATTN_ARG_SEQS)
+    for (int b = 0; b < v.B; ++b) { a.nF[b] = c->nF[b]; a.nQ[b] = c->nQ[b]; }
+  HIPCHK(c, launch_tree_attend(a, v.D, c->kt, st));
+  c->tree_nodes[layer] = n_tree; c->tree_len[layer] = c->n_assigned;
+  if (c->jobs_next < c->jobs.size()) return pump_transfers(c, 1);
+  return TKV_OK;
+}
+
+tkv_status tkv_verify_tree(tkv_cache* c, const tkv_tree_walk* w, void* hip_stream) {
+  if (!c) return TKV_EINVAL;
+  if (!w || !w->parents || !w->tokens || !w->p || !w->u_accept || !w->u_draw || !w->path || !w->n_path || !w->next)
+    return fail(c, TKV_EINVAL, "tkv_verify_tree: NULL argument");
+  if (w->n_tree < 1 || w->n_tree > TKV_TREE_MAX || w->vocab < 1 || w->vocab > (1 << 30) || w->prob_dtype < TKV_F32 || w->prob_dtype > TKV_F16)
+    return fail(c, TKV_EINVAL, "tkv_verify_tree: bad sizes or type (1 to %d nodes)", TKV_TREE_MAX);
+  if (w->p_stride < w->vocab || (w->q && w->q_stride < w->vocab)) return fail(c, TKV_EINVAL, "tkv_verify_tree: rows overlap");
+  ON_DEVICE(c);
+  hipStream_t st = (hipStream_t)hip_stream;
+  const int B = c->dv.B;
+  if (!c->walk_arrived) {
+    double* part = nullptr;
+    int* arrived = nullptr;
+    if (!dalloc(c, part, (size_t)B * WALK_MAX_PARTS) || !dalloc(c, arrived, (size_t)B)) return fail(c, TKV_ENOMEM, "tkv_verify_tree: no device memory for the scratch");
+    HIPCHK(c, launch_walk_init(arrived, B, st));
+    c->walk_part = part; c->walk_arrived = arrived;
+  }
+  WalkArgs a{};
+  a.parents = w->parents; a.tokens = w->tokens; a.p = (const char*)w->p; a.q = (const char*)w->q; a.u = w->u_accept; a.u_draw = w->u_draw;
+  a.path = w->path; a.n_path = w->n_path; a.next = w->next; a.part = c->walk_part; a.arrived = c->walk_arrived;
+  a.p_stride = w->p_stride; a.q_stride = w->q_stride; a.B = B; a.n = w->n_tree; a.vocab = w->vocab; a.W = walk_parts(B, w->vocab, c->cus);
+  HIPCHK(c, launch_walk(a, w->prob_dtype, st));
+  return TKV_OK;
+}
+
+tkv_status tkv_accept_tree(tkv_cache* c, int32_t n_tree, const int32_t* path, int32_t n_path, const void* q_all, int32_t* n_kept, void* hip_stream) {
+  if (!c) return TKV_EINVAL;
+  if (n_kept) *n_kept = 0;
+  if (n_tree < 1 || n_tree > TKV_TREE_MAX || n_path < 0 || n_path > TKV_TREE_MAX || (n_path > 0 && !path))
+    return fail(c, TKV_EINVAL, "tkv_accept_tree: bad argument (1 to %d nodes)", TKV_TREE_MAX);
+  if (const char* why = tree_refusal(c)) return fail(c, TKV_EINVAL, "tkv_accept_tree: %s", why);
+  if (c->plan_pending) return fail(c, TKV_ESTATE, "tkv_accept_tree: a tier plan is pending; call tkv_migrate first");
+  const int n = common_length(c);
+  if (n < 0 || n != c->n_assigned) return fail(c, TKV_ESTATE, "tkv_accept_tree: layers differ in length");
+  if (n_tree > n - c->n_at_plan)
+    return fail(c, TKV_ESTATE, "tkv_accept_tree: %d nodes, but only %d positions were appended since the last tkv_migrate", n_tree, n - c->n_at_plan);
+  DevView& v = c->dv;
+  const bool scored = q_all && n_path > 0;
+  if (scored)
+    for (int l = 0; l < v.L; ++l)
+      if (c->tree_nodes[l] != n_tree || c->tree_len[l] != n)
+        return fail(c, TKV_ESTATE, "tkv_accept_tree: layer %d has not been attended with this tree, its queries' weights are not known", l);
+  ON_DEVICE(c);
+  hipStream_t st = (hipStream_t)hip_stream;
+  const int B = v.B, base = n - n_tree;
+  if (!c->info_tree) {
+    int* info = nullptr;
+    int* pin = (int*)pin_alloc(c, (size_t)2 * B * sizeof(int));
+    if (!pin || !dalloc(c, info, (size_t)2 * B)) return fail(c, TKV_ENOMEM, "tkv_accept_tree: no memory for the counts");
+    c->info_tree = info; c->pin_info = pin;
+  }
+  if (scored && !c->gain_tree) {
+    // a float per layer and list entry, for as many layers at a time as 64 MiB hold
+    c->gain_stride = (v.Nmax + 31) / 32 * 32 + 64;
+    const size_t row = (size_t)B * c->gain_stride * sizeof(float);
+    const int nl = (int)std::min<size_t>(v.L, std::max<size_t>(1, ((size_t)64 << 20) / row));
+    float* p = nullptr;
+    if (!dalloc(c, p, nl * row / sizeof(float))) return fail(c, TKV_ENOMEM, "tkv_accept_tree: no device memory for the scores' scratch");
+    c->gain_tree = p; c->gain_layers = nl;
+  }
+  HIPCHK(c, launch_accept_check(v, base, n_tree, path, n_path, c->info_tree, st));
+  HIPCHK(c, hipMemcpyAsync(c->pin_info, c->info_tree, (size_t)2 * B * sizeof(int), hipMemcpyDeviceToHost, st));
+  HIPCHK(c, hipStreamSynchronize(st));
+  int keep = 0;
+  for (int b = 0; b < B; ++b) {
+    if (c->pin_info[2 * b] < 0) return fail(c, TKV_EINVAL, "tkv_accept_tree: the path of sequence %d is not an ascending list of the tree's nodes", b);
+    keep = std::max(keep, c->pin_info[2 * b]);
+  }
+  HIPCHK(c, launch_accept(v, base, n_tree, keep, path, n_path, c->info_tree, st));
+  int max_rows = 0;
+  bool left = false;                                     // gaps at the cache's end
+  for (int b = 0; b < B; ++b) {
+    const int kept = c->pin_info[2 * b], slots = c->pin_info[2 * b + 1];
+    c->nF[b] += kept - slots; c->free0[b] += slots - kept;
+    c->ntier[0] += kept - slots; c->ntier[3] += (keep - kept) - (n_tree - slots);
+    max_rows = std::max(max_rows, c->nF[b] + c->nQ[b]);
+    c->gaps += (keep - kept) - (n_tree - slots);
+    left = left || kept < keep;
+  }
+  c->n_assigned = base + keep;
+  std::fill(c->len.begin(), c->len.end(), base + keep);
+  c->whole_from = left ? base + keep : c->gaps > 0 ? std::min(c->whole_from, base) : 0;
+  std::fill(c->tree_nodes.begin(), c->tree_nodes.end(), 0);
+  if (n_kept) *n_kept = keep;
+  if (!scored || keep == 0) return TKV_OK;
+  // rows on their way to the staging buffer still have their bits in their old slots
+  bool moving = false;
+  for (int l = 0; l < v.L; ++l) moving = moving || c->layer_wait[l];
+  for (int l = 0; l < v.L; l += c->gain_layers) {
+    const size_t lrows = (size_t)l * B * v.Hkv;
+    TreeScoreArgs a{};
+    a.fpK = v.fpK + lrows * v.capP * v.D * v.es; a.c2K = v.c2K + lrows * v.cap2 * v.cb; a.s2K = v.s2K + lrows * v.cap2 * v.sb;
+    a.q = (const char*)q_all + (size_t)l * B * n_tree * v.Hq * v.D * v.es;
+    a.path = path; a.n_path = n_path; a.kept = c->info_tree;
+    a.f_loc = moving ? v.f_loc_old : v.f_loc; a.f_pos = v.f_pos; a.q_loc = v.q_loc; a.q_pos = v.q_pos; a.cnt = v.cnt;
+    a.stat_stride = c->tree_cap * c->G; a.stat = c->stat_tree + lrows * a.stat_stride;
+    a.vnorm = v.vnorm ? v.vnorm + lrows * v.Nmax : nullptr;
+    a.gain = c->gain_tree; a.score = v.score; a.stride = c->gain_stride; a.layers = std::min(c->gain_layers, v.L - l);
+    a.B = B; a.Hq = v.Hq; a.Hkv = v.Hkv; a.G = c->G; a.n = n_tree; a.Nmax = v.Nmax; a.capF = v.capP; a.cap2 = v.cap2; a.cb = v.cb; a.sb = v.sb; a.t2fmt = v.t2fmt;
+    a.scale2 = c->softmax_scale * 1.4426950408889634f; a.score_scale = c->score_scale;
+    HIPCHK(c, launch_tree_scores(a, v.D, c->kt, max_rows, st));
+  }
+  return TKV_OK;
+}
+
+tkv_status tkv_commit_tree(tkv_cache* c, const tkv_tree_walk* w, const void* q_all, int32_t* n_kept, void* hip_stream) {
+  if (n_kept) *n_kept = 0;
+  const tkv_status s = tkv_verify_tree(c, w, hip_stream);
+  return s != TKV_OK ? s : tkv_accept_tree(c, w->n_tree, w->path, w->n_tree, q_all, n_kept, hip_stream);
 }
 
 tkv_status tkv_decode_step(tkv_cache* c, const void* k_all, const void* v_all, const void* q_all, void* out_all,
@@ -1252,6 +1477,7 @@ tkv_status tkv_migrate(tkv_cache* c, void* hip_stream) {
   }
   c->plan_pending = false;
   c->n_at_plan = n;
+  c->gaps = 0; c->whole_from = 0;
   c->st.n_migrate++;
   c->st.migrate_ms += std::chrono::duration<double, std::milli>(std::chrono::steady_clock::now() - t0).count();
   return TKV_OK;
