@@ -85,6 +85,7 @@ struct tkv_cache {
   // drafted trees: scratch for trees of up to tree_cap nodes, and which layers have been attended with which tree since the last
   // append or accept (their columns' statistics are in stat_tree)
   int tree_cap = 0;
+  size_t tree_cols = 0;            // (pair, split, column)s that the partials have room for
   float* ml_tree = nullptr; float* po_tree = nullptr; float2* stat_tree = nullptr; int* here_tree = nullptr;
   float* gain_tree = nullptr;      // kept queries' weights, gain_layers layers at a time
   int gain_layers = 0, gain_stride = 0;
@@ -1037,14 +1038,30 @@ const char* tree_refusal(const tkv_cache* c) {
     return "not available with the redundancy-penalised scorers (a row's redundancy is taken against the row appended before it)";
   return nullptr;
 }
-// splits of a pair's tiles: workgroups for all compute units, of four tiles or more
-int tree_splits(const tkv_cache* c, int n) {
+// A workgroup's shape and the splits of a pair's tiles, from the longest lists: those of the least time, in us.  A round of workgroups takes
+// TREE_BEGIN (and as much again for every block of 16 columns that a wave has) for beginning and end and so much for every tile (16-bit rows:
+// by the wave's blocks, or at the memory's rate if that is less); with more than one split every share is written and read back, and
+// k_tree_merge comes on top.
+constexpr int TREE_MAX_SPLITS = 64;
+constexpr double TREE_BEGIN = 6.0, TREE_BLOCK = 1.0, TREE_MERGE = 4.5, TREE_SHARE_BYTES = 4.0e6, TREE_ROW_BYTES = 5.5e6;
+struct TreePlan { TreeShape shape; int S; };
+TreePlan tree_plan(const tkv_cache* c, int n, int n_list) {
   const DevView& v = c->dv;
-  const TreeShape s = tree_shape(v.D, c->kt, n * c->G);
-  const int tr = tree_tile_rows(s), units = tree_units(c->kt, s, c->cus), per = v.B * v.Hkv * s.groups;
-  int tiles = 1;
-  for (int b = 0; b < v.B; ++b) tiles = std::max(tiles, (c->nF[b] + tr - 1) / tr + (c->nQ[b] + tr - 1) / tr);
-  return std::max(1, std::min({units / per, (tiles + 3) / 4, 64}));
+  const int C = n * c->G, pairs = v.B * v.Hkv;
+  const double share = (double)pairs * C * v.D * 8 / TREE_SHARE_BYTES, a_block = c->cfg.out_dtype == TKV_F32 ? 0.8 : 0.45;
+  TreePlan best{};
+  double least = 1e30;
+  TreeShape s;
+  for (int which = 0; tree_shape(c->kt, C, which, s); ++which) {
+    const int tr = 32 * s.waves_r, tiles = (n_list + tr - 1) / tr + 1;
+    const double tile = c->kt == 0 ? 3.0 : std::max(0.5 + a_block * s.blocks, (double)tr * v.D * 4 * c->cus / TREE_ROW_BYTES * (s.groups > 1 ? 0.7 : 1.0));
+    for (int S = 1; S <= std::min(TREE_MAX_SPLITS, tiles); ++S) {
+      const double cost = (double)((pairs * (int64_t)S * s.groups + c->cus - 1) / c->cus) * ((tiles + S - 1) / S * tile + TREE_BEGIN + TREE_BLOCK * s.blocks) + (S > 1 ? TREE_MERGE + share * S : 0.0);
+      if (cost < least) { least = cost; best = {s, S}; }
+    }
+    if (s.groups == 1) break;                            // (a wider one has nothing more to do)
+  }
+  return best;
 }
 // Scratch for trees of n nodes: partials for as many splits as there may be, statistics of all layers.
 tkv_status tree_scratch(tkv_cache* c, int n) {
@@ -1054,9 +1071,13 @@ tkv_status tree_scratch(tkv_cache* c, int n) {
   while (cap < n) cap *= 2;
   size_t cols = 0;                                       // (pair, split, column)s
   for (int m = 1; m <= cap; ++m) {
-    const TreeShape s = tree_shape(v.D, c->kt, m * c->G);
-    const size_t pairs = (size_t)v.B * v.Hkv, S = std::min<size_t>(64, std::max<size_t>(1, (size_t)tree_units(c->kt, s, c->cus) / (pairs * s.groups)));
-    cols = std::max(cols, S == 1 ? 0 : pairs * S * m * c->G);
+    // (the rule's splits are not monotonous in the lists' length)
+    int most = 1;
+    for (int len = 32; ; len = std::min(v.Nmax, len + std::max(32, len / 8))) {
+      most = std::max(most, tree_plan(c, m, len).S);
+      if (len == v.Nmax || v.Nmax <= 32) break;
+    }
+    cols = std::max(cols, (size_t)v.B * v.Hkv * most * m * c->G);
   }
   float *ml = nullptr, *po = nullptr;
   float2* stat = nullptr;
@@ -1064,7 +1085,7 @@ tkv_status tree_scratch(tkv_cache* c, int n) {
   if (!dalloc(c, ml, cols * 2) || !dalloc(c, po, cols * v.D) || !dalloc(c, stat, (size_t)v.L * v.B * v.Hq * cap) || !dalloc(c, here, (size_t)v.B * cap))
     return fail(c, TKV_ENOMEM, "tkv_attend_tree: no device memory for the scratch of %d nodes", cap);
   c->ml_tree = ml; c->po_tree = po; c->stat_tree = stat; c->here_tree = here;
-  c->tree_cap = cap;
+  c->tree_cap = cap; c->tree_cols = cols;
   std::fill(c->tree_nodes.begin(), c->tree_nodes.end(), 0);    // (the statistics start anew)
   return TKV_OK;
 }
@@ -1082,6 +1103,8 @@ tkv_status tkv_attend_tree(tkv_cache* c, int32_t layer, const void* q, const int
   ON_DEVICE(c);
   tkv_status s = tree_scratch(c, n_tree);
   if (s != TKV_OK) return s;
+  int longest = 0;
+  for (int b = 0; b < c->dv.B; ++b) longest = std::max(longest, c->nF[b] + c->nQ[b]);
   hipStream_t st = (hipStream_t)hip_stream;
   uint64_t old_mask = 0;
   s = settle_rows(c, layer, 1, false, st, old_mask);
@@ -1097,7 +1120,9 @@ tkv_status tkv_attend_tree(tkv_cache* c, int32_t layer, const void* q, const int
   a.cnt = v.cnt; a.part_ml = c->ml_tree; a.part_o = c->po_tree; a.here = c->here_tree;
   a.B = v.B; a.Hq = v.Hq; a.Hkv = v.Hkv; a.G = c->G; a.n = n_tree; a.C = n_tree * c->G;
   a.stat_stride = c->tree_cap * c->G; a.stat = c->stat_tree + lrows * a.stat_stride;
-  a.S = tree_splits(c, n_tree); a.groups = tree_shape(v.D, c->kt, a.C).groups;
+  const TreePlan plan = tree_plan(c, n_tree, longest);
+  a.S = std::max(1, std::min(plan.S, (int)(c->tree_cols / ((size_t)v.B * v.Hkv * a.C)))); a.groups = plan.shape.groups;
+  a.waves_c = plan.shape.waves_c; a.blocks = plan.shape.blocks;
   a.Nmax = v.Nmax; a.capF = v.capP; a.cap2 = v.cap2; a.cb = v.cb; a.sb = v.sb; a.t2fmt = v.t2fmt; a.out_kind = c->cfg.out_dtype;
   a.scale2 = c->softmax_scale * 1.4426950408889634f;
   if (v.B <= ATTN_ARG_SEQS)

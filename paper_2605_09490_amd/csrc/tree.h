@@ -22,6 +22,7 @@ struct TreeArgs {
   int* here;                          // [B][n] whether a node is there
   int B, Hq, Hkv, G, n, C;            // C = n * G columns of a kv head, column = node * G + head of the group
   int S, groups;                      // splits of a pair's tiles, groups of columns
+  int waves_c, blocks;                // the workgroup's shape (TreeShape)
   int Nmax, capF, cap2, cb, sb, t2fmt, out_kind;
   float scale2;                       // softmax_scale * log2 e
   int nF[ATTN_ARG_SEQS], nQ[ATTN_ARG_SEQS];
@@ -43,10 +44,10 @@ struct TreeScoreArgs {
   float scale2, score_scale;
 };
 
-struct TreeShape { int waves_c, waves_r, groups; };          // waves side by side over columns and over rows, groups of columns
-TreeShape tree_shape(int D, int kt, int C);
-int tree_tile_rows(const TreeShape& s);
-int tree_units(int kt, const TreeShape& s, int cus);         // workgroups that run at once
+// Shapes of a workgroup: waves side by side over columns and over rows, a wave's blocks of 16 columns; groups of columns that a tree of C
+// columns then takes.  The narrowest comes first; false: there are no more.
+struct TreeShape { int waves_c, waves_r, blocks, groups; };
+bool tree_shape(int kt, int C, int which, TreeShape& s);
 hipError_t launch_tree_attend(const TreeArgs& a, int D, int kt, hipStream_t st);
 hipError_t launch_tree_scores(const TreeScoreArgs& a, int D, int kt, int max_rows, hipStream_t st);
 

@@ -26,7 +26,7 @@ extern "C" hipError_t hipLaunchKernel(const void* f, dim3 grid, dim3 block, void
     if (a.S > 1) CHECK(inside(a.part_ml, pairs * a.S * 2 * a.C * 4) && inside(a.part_o, pairs * a.S * a.C * D * 4));
     CHECK(a.stat_stride >= a.C && inside(a.stat, pairs * a.stat_stride * 8) && inside(a.here, (size_t)a.B * a.n * 4));
     if (is("k_tree_attend")) { CHECK(grid.x >= pairs * a.S * a.groups && grid.x % 8 == 0); g_trees.push_back(a); g_order += 'a'; }
-    else { CHECK(a.S > 1 && grid.x * 4 >= (unsigned)a.C && grid.y == pairs); g_order += 'm'; }
+    else { CHECK(a.S > 1 && grid.x * 16 >= (unsigned)a.C && grid.y == pairs); g_order += 'm'; }
     return hipSuccess;
   }
   if (is("k_tree_scores") || is("k_tree_gain")) {
