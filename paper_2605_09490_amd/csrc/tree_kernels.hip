@@ -876,8 +876,8 @@ __global__ __launch_bounds__(64 * WC * WR) void k_tree_attend_f32(const TreeArgs
 // ---- the kept queries' weights ---------------------------------------------------------------------------------------------
 // Grid (runs of 128 list entries, B, layers).  A wave has 32 rows of list F or list Q, for one kv head after the other, and the kept
 // columns of that head in blocks of 32.  Bound by the K rows, which arrive once; 4 waves a workgroup, each on its own.
-template <int D, int KT>
-__global__ __launch_bounds__(256) void k_tree_scores(const TreeScoreArgs a) {
+template <int D, int KT, int QM>
+__global__ __launch_bounds__(256, 2) void k_tree_scores(const TreeScoreArgs a) {
   constexpr int ES = KT == KT_F32 ? 4 : 2, RB = D * ES, PPR = RB / 16, NPT = 32 * PPR / 64;
   constexpr int NG = D / 32, NQF = KT == KT_F32 ? D / 8 : D / 16, KP = Pitch<D, ES>::K;
   __shared__ __attribute__((aligned(16))) char sm_k[4][32 * KP];
@@ -931,6 +931,20 @@ __global__ __launch_bounds__(256) void k_tree_scores(const TreeScoreArgs a) {
       }
     };
     load();
+    // A block's queries and statistics are asked for while the one before it is weighed
+    u32x4 qf[NQF];
+    float2 st;
+    int j = 0;                                             // the column's token
+    const auto load_q = [&](int kvh, int c0) __attribute__((always_inline)) {
+      const int c = c0 + ln < kept * a.G ? c0 + ln : kept * a.G - 1, g = c - c / a.G * a.G;
+      j = c / a.G;
+      const int node = a.path[(size_t)b * a.n_path + j];
+      st = a.stat[(lb * a.Hkv + kvh) * a.stat_stride + node * a.G + g];
+      const char* q = (const char*)a.q + ((lb * a.n + node) * a.Hq + kvh * a.G + g) * RB + 16 * h;
+#pragma unroll
+      for (int i = 0; i < NQF; ++i) qf[i] = ((const PackedU32x4*)(q + 32 * i))->v;
+    };
+    load_q(0, 0);
     for (int kvh = 0; kvh < a.Hkv; ++kvh) {
       // (a wave's LDS accesses are served in order: the last head's reads come before these writes)
 #pragma unroll
@@ -960,13 +974,6 @@ __global__ __launch_bounds__(256) void k_tree_scores(const TreeScoreArgs a) {
       for (int r = 0; r < 16; ++r) own[r] = 0.f;
       for (int c0 = 0; c0 < kept * a.G; c0 += 32) {
         const bool on = c0 + ln < kept * a.G;
-        const int c = on ? c0 + ln : kept * a.G - 1, j = c / a.G, g = c - j * a.G;
-        const int node = a.path[(size_t)b * a.n_path + j];
-        const float2 st = a.stat[(lb * a.Hkv + kvh) * a.stat_stride + node * a.G + g];
-        const char* q = (const char*)a.q + ((lb * a.n + node) * a.Hq + kvh * a.G + g) * RB + 16 * h;
-        u32x4 qf[NQF];
-#pragma unroll
-        for (int i = 0; i < NQF; ++i) qf[i] = ((const PackedU32x4*)(q + 32 * i))->v;
         f32x16 s = zero16();
         if constexpr (KT == KT_F32) {
 #pragma unroll
@@ -998,10 +1005,13 @@ __global__ __launch_bounds__(256) void k_tree_scores(const TreeScoreArgs a) {
         }
         // the column's token sees entries up to its own; the kept nodes are the last `kept` entries of list F
         const int lim = MODE == R_FULL ? nF - kept + j + 1 : src.n;
+        const float2 of = st;
+        if (c0 + 32 < kept * a.G) load_q(kvh, c0 + 32);
+        else if (kvh + 1 < a.Hkv) load_q(kvh + 1, 0);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int e = e0 + 8 * (r / 4) + 4 * h + r % 4;
-          const float w = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale2, -st.x)) * st.y;
+          const float w = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale2, -of.x)) * of.y;
           own[r] += on && e < lim ? w : 0.f;
         }
       }
@@ -1030,8 +1040,7 @@ __global__ __launch_bounds__(256) void k_tree_scores(const TreeScoreArgs a) {
     rows(std::integral_constant<int, R_FULL>{}, src, a.f_pos + (size_t)b * a.Nmax, tile * 32);
   } else {
     const RowSrc src{a.c2K + pl * a.cap2 * a.cb, nullptr, a.s2K + pl * a.cap2 * a.sb, nullptr, a.q_loc + (size_t)b * a.Nmax, nQ, a.cap2, a.cb, a.sb};
-    if (a.t2fmt == 0) rows(std::integral_constant<int, R_INT8>{}, src, a.q_pos + (size_t)b * a.Nmax, (tile - tF) * 32);
-    else rows(std::integral_constant<int, R_INT4>{}, src, a.q_pos + (size_t)b * a.Nmax, (tile - tF) * 32);
+    rows(std::integral_constant<int, QM>{}, src, a.q_pos + (size_t)b * a.Nmax, (tile - tF) * 32);
   }
 }
 
@@ -1070,7 +1079,8 @@ hipError_t tree_scores_by_type(const TreeScoreArgs& a, int max_rows, hipStream_t
   }                                                                                                                     \
   template <>                                                                                                           \
   hipError_t tree_scores_by_type<D_, KT_>(const TreeScoreArgs& a, int max_rows, hipStream_t st) {                       \
-    hipLaunchKernelGGL((k_tree_scores<D_, KT_>), dim3((unsigned)(max_rows + 127) / 128 + 1, a.B, a.layers), dim3(256), 0, st, a); \
+    const dim3 grid((unsigned)(max_rows + 127) / 128 + 1, a.B, a.layers);                                               \
+    hipLaunchKernelGGL((a.t2fmt == 0 ? k_tree_scores<D_, KT_, R_INT8> : k_tree_scores<D_, KT_, R_INT4>), grid, dim3(256), 0, st, a); \
     return hipGetLastError();                                                                                           \
   }
 #if TKV_TREE_PART == 0
