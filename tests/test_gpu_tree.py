@@ -561,6 +561,29 @@ def test_two_handles_at_once():
         p.close()
 
 
+@pytest.mark.parametrize("dtype,t2,D,full,coded", [
+    ("bf16", "int8_row", 128, 1e30, 1e30), ("bf16", "int8_row", 128, 1e-30, 1e-30), ("bf16", "int8_row", 64, 1e25, 1e-25), ("bf16", "int8_row", 128, 1e-25, 1e25),
+    ("bf16", "int4_g32", 128, 1e-3, 1e3), ("bf16", "int4_g32", 64, 1e20, 1.0), ("f16", "int8_row", 128, 1e4, 1e-4), ("f16", "int8_row", 64, 1e-4, 1e4),
+    ("f16", "int4_g32", 128, 1e-3, 1e3), ("f32", "int8_row", 64, 1e25, 1e-25)])
+def test_values_of_any_size(dtype, t2, D, full, coded):
+    """V rows far apart in size by tier: what a weight is multiplied with must neither overflow nor lose it.  To the bound of the 2-norm
+    above comes what is lost below 2^-126: with weights of at least 2^-4 for a column's largest, 3 products (a weight's terms) of each of
+    N rows lose less than 2^-126 each, so an output less than 3 N 2^-122."""
+    p = Both(91, Hq=10, Hkv=2, D=D, B=1, ctx=0, dtype=dtype, t2=t2, room=260, L=1)
+    n, N = 12, 200
+    tiers = np.where(np.arange(N) % 3 == 0, 2, 0).astype(np.uint8)[None]
+    tiers[:, -8:] = 0
+    size = torch.from_numpy(np.where(tiers[0] == 2, coded, full)).cuda()[None, :, None, None]
+    p.append(0, p.rows(N, 2), (p.rows(N, 2).double() * size).to(DT[dtype]))
+    p.force(tiers)
+    p.append(0, p.rows(n, 2), (p.rows(n, 2).double() * full).to(DT[dtype]))
+    parents, q = tree(p.rng, 1, n, "tree"), p.rows(n, 10)
+    got, ref = f64(p.gpu.attend_tree(0, q, torch.from_numpy(parents).cuda())), p.orc.attend_tree(0, f64(q), parents)
+    assert np.isfinite(got).all()
+    assert np.linalg.norm(got - ref) <= 3e-6 * np.linalg.norm(ref) + np.sqrt(ref.size) * 3 * (N + n) * 2.0 ** -122
+    p.close()
+
+
 @pytest.mark.parametrize("offset", [1, 4])
 def test_queries_that_begin_between_16_byte_boundaries(offset):
     p = Both(73, ctx=80, L=1)
