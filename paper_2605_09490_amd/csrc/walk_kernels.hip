@@ -12,7 +12,7 @@
 
 namespace tkv {
 
-constexpr int WALK_THREADS = 512, WALK_WAVES = WALK_THREADS / 64;
+constexpr int WALK_THREADS = 1024, WALK_WAVES = WALK_THREADS / 64;
 
 template <int PT>
 __device__ __forceinline__ double prob(const char* row, long long x) {
@@ -45,23 +45,51 @@ struct Residual {
   }
 };
 
-// sum of elements lo .. hi - 1, by the lanes t, t + stride, ... of `stride`
-template <int PT>
-__device__ __forceinline__ double part_sum(const Residual& r, int lo, int hi, int t, int stride) {
-  constexpr int ES = PT == KT_F32 ? 4 : 2, VE = 16 / ES;
-  double s = 0.0;
-#pragma unroll 2
-  for (int x = lo + t * VE; x < hi; x += stride * VE) {
-    if (x + VE <= hi) {
-      const u32x4 pv = ((const PackedU32x4*)(r.p + (size_t)x * ES))->v;
-      u32x4 qv = {0u, 0u, 0u, 0u};
-      if (r.q) qv = ((const PackedU32x4*)(r.q + (size_t)x * ES))->v;
+// elements x .. of a row, as `at` makes them, added up
+template <int PT, int VE>
+__device__ __forceinline__ double piece_sum(const Residual& r, const u32x4& pv, const u32x4& qv, int x) {
+  double v[VE];
 #pragma unroll
-      for (int e = 0; e < VE; ++e) s += r.at(prob_of<PT>(pv, e), prob_of<PT>(qv, e), x + e);
+  for (int e = 0; e < VE; ++e) v[e] = prob_of<PT>(pv, e);
+  for (int k = 0; k < r.subs; ++k) {
+    if (r.q) {
+      const double total = r.total[k];
+#pragma unroll
+      for (int e = 0; e < VE; ++e) v[e] = fmax(v[e] - total * prob_of<PT>(qv, e), 0.0);
     } else {
-      for (int e = x; e < hi; ++e) s += r.at(prob<PT>(r.p, e), r.q ? prob<PT>(r.q, e) : 0.0, e);
+      const int out = r.out[k] - x;
+#pragma unroll
+      for (int e = 0; e < VE; ++e) v[e] = out == e ? 0.0 : v[e];
     }
   }
+  double s = 0.0;
+#pragma unroll
+  for (int e = 0; e < VE; ++e) s += v[e];
+  return s;
+}
+// sum of elements lo .. hi - 1, by the lanes t, t + stride, ... of `stride`.  32 elements of a lane (of either row) are on their way at
+// once: one workgroup alone waits for memory otherwise.
+template <int PT>
+__device__ __forceinline__ double part_sum(const Residual& r, int lo, int hi, int t, int stride) {
+  constexpr int ES = PT == KT_F32 ? 4 : 2, VE = 16 / ES, MANY = 32 / VE;
+  double s = 0.0;
+  const int whole = lo + (hi > lo ? (hi - lo) / VE * VE : 0);
+  for (int x = lo + t * VE; x < whole; x += MANY * stride * VE) {
+    u32x4 pv[MANY], qv[MANY];
+#pragma unroll
+    for (int i = 0; i < MANY; ++i) {
+      const int y = x + i * stride * VE < whole ? x + i * stride * VE : x;
+      pv[i] = ((const PackedU32x4*)(r.p + (size_t)y * ES))->v;
+      qv[i] = u32x4{0u, 0u, 0u, 0u};
+      if (r.q) qv[i] = ((const PackedU32x4*)(r.q + (size_t)y * ES))->v;
+    }
+#pragma unroll
+    for (int i = 0; i < MANY; ++i) {
+      const int y = x + i * stride * VE;
+      if (y < whole) s += piece_sum<PT, VE>(r, pv[i], qv[i], y);
+    }
+  }
+  if (whole + t < hi) s += r.at(prob<PT>(r.p, whole + t), r.q ? prob<PT>(r.q, whole + t) : 0.0, whole + t);      // (fewer than VE of them)
   return s;
 }
 __device__ __forceinline__ double wave_sum_f64(double x) {
@@ -73,8 +101,8 @@ __device__ __forceinline__ double wave_sum_f64(double x) {
 template <int PT>
 __global__ __launch_bounds__(WALK_THREADS) void k_walk(const WalkArgs a) {
   constexpr int ES = PT == KT_F32 ? 4 : 2;
-  __shared__ double sm_total[TREE_MAX], sm_part[WALK_MAX_PARTS], sm_wave[WALK_WAVES], sm_u[TREE_MAX], sm_p[TREE_MAX], sm_q[TREE_MAX];
-  __shared__ int sm_out[TREE_MAX], sm_path[TREE_MAX], sm_tok[TREE_MAX];
+  __shared__ double sm_total[TREE_MAX], sm_part[WALK_MAX_PARTS], sm_wave[WALK_WAVES];
+  __shared__ int sm_out[TREE_MAX], sm_path[TREE_MAX];
   __shared__ int sm_cur, sm_subs, sm_want, sm_last, sm_token, sm_chunk;
   __shared__ double sm_base;
   const int b = blockIdx.y, w0 = blockIdx.x, t = threadIdx.x, lane = t & 63, wave = t >> 6, n = a.n;
@@ -82,7 +110,8 @@ __global__ __launch_bounds__(WALK_THREADS) void k_walk(const WalkArgs a) {
   const auto row = [&](const char* base, long long stride, int node) { return base + ((size_t)b * n + node) * (size_t)stride * ES; };
 
   // wave 0: what the tests need of every node, nodes `lane` and `lane + 64`
-  int par[2] = {-1, -1};
+  int par[2] = {-1, -1}, tok[2] = {-1, -1};
+  double node_u[2] = {0.0, 0.0}, node_p[2] = {0.0, 0.0}, node_q[2] = {0.0, 0.0};
   if (wave == 0) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -92,10 +121,10 @@ __global__ __launch_bounds__(WALK_THREADS) void k_walk(const WalkArgs a) {
       if (i < n) {
         const int x = a.tokens[b * n + i];
         const bool ok = par[k] >= 0 && x >= 0 && x < a.vocab;
-        sm_tok[i] = x;
-        sm_u[i] = (double)a.u[b * n + i];
-        sm_p[i] = ok ? prob<PT>(row(a.p, a.p_stride, par[k]), x) : 0.0;
-        sm_q[i] = ok && a.q ? prob<PT>(row(a.q, a.q_stride, par[k]), x) : 0.0;
+        tok[k] = x;
+        node_u[k] = (double)a.u[b * n + i];
+        if (ok) node_p[k] = prob<PT>(row(a.p, a.p_stride, par[k]), x);
+        if (ok && a.q) node_q[k] = prob<PT>(row(a.q, a.q_stride, par[k]), x);
         sm_path[i] = -1;
       }
     }
@@ -106,6 +135,13 @@ __global__ __launch_bounds__(WALK_THREADS) void k_walk(const WalkArgs a) {
   // Walk state, the same in all lanes of wave 0
   int cur = 0, last = 0, subs = 0, depth = 1;
   double total = 1.0;
+  // a node's value, from its lane
+  const auto int_of = [](const int (&v)[2], int i) { return __builtin_amdgcn_readlane(i < 64 ? v[0] : v[1], i & 63); };
+  const auto value_of = [](const double (&v)[2], int i) {
+    const uint64_t x = __builtin_bit_cast(uint64_t, i < 64 ? v[0] : v[1]);
+    const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)x, i & 63), hi = __builtin_amdgcn_readlane((uint32_t)(x >> 32), i & 63);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+  };
   // On from here: up to a rejection whose residual has to be summed (q given; subs counts it then), or to the end.
   const auto walk = [&]() -> bool {
     for (;;) {
@@ -113,9 +149,10 @@ __global__ __launch_bounds__(WALK_THREADS) void k_walk(const WalkArgs a) {
       if (!(lo | hi)) return false;
       const int i = lo ? __builtin_ctzll(lo) : 64 + __builtin_ctzll(hi);
       last = i;
-      const Residual r{a.p, a.q, subs, sm_total, sm_out};
-      const double qv = a.q ? sm_q[i] : 1.0, left = r.at(sm_p[i], sm_q[i], sm_tok[i]);
-      if (sm_u[i] * total * qv < left) {
+      const double qv = a.q ? value_of(node_q, i) : 1.0;
+      double left = value_of(node_p, i);
+      if (a.q) left = Residual{a.p, a.q, subs, sm_total, sm_out}.at(left, qv, 0);
+      if (value_of(node_u, i) * total * qv < left) {
         cur = i; subs = 0; total = 1.0;
         if (lane == 0) sm_path[depth] = i;
         ++depth;
@@ -125,7 +162,13 @@ __global__ __launch_bounds__(WALK_THREADS) void k_walk(const WalkArgs a) {
         return true;
       } else {
         const double mass = total - left;
-        if (mass > 0.0) { if (lane == 0) sm_out[subs] = sm_tok[i]; ++subs; total = mass; }
+        if (mass > 0.0) {
+          const int x = int_of(tok, i);
+          if (lane == 0) sm_out[subs] = x;
+#pragma unroll
+          for (int k = 0; k < 2; ++k) node_p[k] = par[k] == cur && tok[k] == x ? 0.0 : node_p[k];
+          ++subs; total = mass;
+        }
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
