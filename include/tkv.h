@@ -248,8 +248,9 @@ tkv_status tkv_decode_step(tkv_cache* c, const void* k_all, const void* v_all, c
  * the tree, to its ancestors and to itself.  The output of a node that is not there is zero, and its rows are nobody's, whatever they
  * hold; the rows and queries of the others must be finite.  Adds nothing to the scores: whether a node stays is not known yet; the
  * softmax statistics that tkv_accept_tree needs stay in the handle until the cache's length changes.  T1 placement is bit-invisible
- * (Prop. 1); outputs agree with those of single-token steps to binary32 rounding, with 16-bit rows to 1e-6 (two 16-bit terms per
- * weight).  The first call, and the first with more than 16, 32 or 64 nodes, allocates scratch (not while its stream is captured).
+ * (Prop. 1).  Outputs in binary32 agree with those of single-token steps to binary32 rounding (a weight is held to 2^-23 beside
+ * 16-bit rows, where its product with a V element is above 2^-122); 16-bit outputs are made with weights rounded to the rows' type.
+ * The first call, and the first with more than 16, 32 or 64 nodes, allocates scratch (not while its stream is captured).
  * EINVAL beyond TKV_TREE_MAX nodes; ESTATE unless the n_tree positions are in the cache of every sequence and were appended after the
  * last tkv_migrate. */
 tkv_status tkv_attend_tree(tkv_cache* c, int32_t layer, const void* q, const int32_t* parents, int32_t n_tree, void* out, void* hip_stream);

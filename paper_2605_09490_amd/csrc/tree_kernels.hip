@@ -41,7 +41,7 @@ __device__ __forceinline__ float max_swap32(float x) {         // maximum over l
   return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
 }
 
-// Two weights as a sum of NT 16-bit terms, each the nearest to what the terms before it left.  Binary32 outputs: three bfloat16
+// Two weights as a sum of NT 16-bit terms, each the nearest to what the terms before it left (16-bit outputs: one).  Binary32 outputs: three bfloat16
 // terms hold a weight whole (two leave up to 2^-18 of it: outputs 1.7e-6 from 64 bits, where binary32 arithmetic is 6e-7), two
 // binary16 terms to 2^-23.
 template <int KT, int NT>
@@ -289,13 +289,23 @@ __device__ __forceinline__ void lds_barrier() {
 // ---- attention, 16-bit rows ----------------------------------------------------------------------------------------------
 // A wave has NB blocks of 16 columns.  S^T = K q^T and O^T = V^T P^T in 16x16x32 products: a lane owns one column of every block (lane & 15;
 // its rows are 16 rb + 4 kb + r, kb = lane / 16), so that maximum, sum and their corrections need no exchange but between the wave's four
-// quarters, and the weights leave the first product as the second one's operand.
+// quarters (and the maximum only where a lane's own logits pass it 2^LAG times), and the weights leave the first product as the second
+// one's operand.  With 32x32x16 products, whose columns come in 32s, five blocks of 32 for 160 columns left one SIMD the load of two.
 // Rows of list F go straight to the LDS (1 KB an instruction: 4 rows of 256 bytes, 8 of 128), two stages in turn: the next tile's are
 // under way while one is computed on.  The LDS order is lane order, so a row's 16-byte pieces are rotated by fetching them so: K rows are
 // read by 16 lanes with a row each, the same piece of all; V rows transposed, four rows x 32 bytes at a time; with a piece's width (V: two)
 // between blocks of 1 KB neither meets a bank twice.  Every stage is an array of its own and the loop is unrolled over them: reads of one do
 // not wait for what is on its way to the other.
-// Rows of list Q come through registers, two tiles ahead, and are widened into the stages.
+// Rows of list Q come through registers, a tile or two ahead, and are widened into the stages.  Their codes are exact in 16 bits, and scales
+// stay outside the products: K's on the logits, V's on the weights, which then go to the matrix cores in binary16 whatever the rows' type
+// (two terms hold a weight to 2^-23, where bfloat16 takes three).
+// Eight waves a workgroup (two a SIMD) and one workgroup a CU.  What bounds it depends: 32 sequences x 16384 in int4, 895 MB, 205 us: the
+// memory (4.4 TB/s; a large copy reads and writes 4.8).  4 x 8201 in binary16, 42 us: the rows at 3 TB/s, beginning, end and the splits'
+// join being 12 of them.  8 x 4133 with 160 columns, 67 us: the matrix cores have 51 GFLOP with three terms a weight, 0.8 PFLOP/s over the
+// launch's 63 us (a large product here: 1.2), and of that time neither leaving out the weights (-16 us), two of three terms (-12) nor the
+// fetches (-8) would free much.  One user's 1422 rows, 15 us a layer: one tile a workgroup, beginning and end.
+// Not kept: the waves of a SIMD in opposite phases (two barriers a tile: 79 us for the 160 columns against 78; one: 83), blocks of columns dealt
+// out 3 / 2 over the waves (126: two bodies of code).
 template <int D>
 struct Block {
   static constexpr int RB = 2 * D, ROWS = 1024 / RB, KPITCH = 1040, VPITCH = 1056, N = 32 / ROWS;      // rows of a block; blocks of 32 rows
@@ -875,7 +885,9 @@ __global__ __launch_bounds__(64 * WC * WR) void k_tree_attend_f32(const TreeArgs
 
 // ---- the kept queries' weights ---------------------------------------------------------------------------------------------
 // Grid (runs of 128 list entries, B, layers).  A wave has 32 rows of list F or list Q, for one kv head after the other, and the kept
-// columns of that head in blocks of 32.  Bound by the K rows, which arrive once; 4 waves a workgroup, each on its own.
+// columns of that head in blocks of 32; 4 waves a workgroup, each on its own.  Bound by the latency of the K rows, which arrive once, and of
+// the queries: eight layers of 8 x 4133 rows (0.49 GB, 101 us at the rate of a copy) take 115 us with two waves a SIMD and the next block's queries asked for early, 137
+// without that, 209 with one wave (both code formats in one kernel); three waves spill (146).
 template <int D, int KT, int QM>
 __global__ __launch_bounds__(256, 2) void k_tree_scores(const TreeScoreArgs a) {
   constexpr int ES = KT == KT_F32 ? 4 : 2, RB = D * ES, PPR = RB / 16, NPT = 32 * PPR / 64;
@@ -1107,6 +1119,7 @@ TKV_TREE_DECLARE(128, KT_BF16) TKV_TREE_DECLARE(128, KT_F16) TKV_TREE_DECLARE(12
 TKV_TREE_DECLARE(64, KT_BF16) TKV_TREE_DECLARE(64, KT_F16) TKV_TREE_DECLARE(64, KT_F32)
 
 // ---- splits joined: D / 4 lanes per (pair, column), eight splits at a time --------------------------------------------------
+// Bound by latency: 21 MB in 6.8 us (9.6 with a wave per column, maximum and sum before the rest).
 template <int D>
 __global__ __launch_bounds__(256) void k_tree_merge(const TreeArgs a) {
   constexpr int LANES = D / 4, COLS = 256 / LANES, MANY = 8;

@@ -5,7 +5,10 @@
 //            a wave gather for all nodes at once; only the sum of a residual, and the draw of the next token, read whole rows.  Every
 //            workgroup walks the tree (the same steps in each) up to the first such sum and takes its part of the row; the last to
 //            arrive adds the parts, walks on, and draws.  Sums and residuals are held in 64 bits: which token is drawn, and whether
-//            one is taken, is decided by comparing them.
+//            one is taken, is decided by comparing them.  Bound by the chain of dependent steps: a gather, a sum, the parts'
+//            meeting, the draw (16 us for one line), and a pass of one workgroup over a row (8 us for 100003 pairs in binary32, with
+//            32 elements of a lane on their way; 16 with four) for every further rejection of a drawn child.  A barrier of a
+//            sequence's workgroups instead would need them all on the chip at once, which nobody can promise.
 //   k_accept_check, k_accept : one workgroup per sequence.  Slots change hands, no row moves.
 #include "device_common.h"
 #include "tree.h"
