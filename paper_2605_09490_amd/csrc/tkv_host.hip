@@ -1055,9 +1055,11 @@ TreePlan tree_plan(const tkv_cache* c, int n, int n_list) {
   TreeShape s;
   for (int which = 0; tree_shape(c->kt, C, which, s); ++which) {
     const int tr = 32 * s.waves_r, tiles = (n_list + tr - 1) / tr + 1;
-    const double tile = c->kt == 0 ? 3.0 : std::max(0.5 + a_block * s.blocks, (double)tr * v.D * 4 * c->cus / TREE_ROW_BYTES * (s.groups > 1 ? 0.7 : 1.0));
+    // (binary32: so many workgroups of one or two waves have room on a CU; a tile is bound by its products)
+    const int units = c->cus * (c->kt == 0 && (s.waves_c == 2 || (s.waves_c == 1 && v.D == 64)) ? 2 : 1);
+    const double tile = c->kt == 0 ? 0.7 + 3.6 * v.D / 128 : std::max(0.5 + a_block * s.blocks, (double)tr * v.D * 4 * c->cus / TREE_ROW_BYTES * (s.groups > 1 ? 0.7 : 1.0));
     for (int S = 1; S <= std::min(TREE_MAX_SPLITS, tiles); ++S) {
-      const double cost = (double)((pairs * (int64_t)S * s.groups + c->cus - 1) / c->cus) * ((tiles + S - 1) / S * tile + TREE_BEGIN + TREE_BLOCK * s.blocks) + (S > 1 ? TREE_MERGE + share * S : 0.0);
+      const double cost = (double)((pairs * (int64_t)S * s.groups + units - 1) / units) * ((tiles + S - 1) / S * tile + TREE_BEGIN + TREE_BLOCK * s.blocks) + (S > 1 ? TREE_MERGE + share * S : 0.0);
       if (cost < least) { least = cost; best = {s, S}; }
     }
     if (s.groups == 1) break;                            // (a wider one has nothing more to do)

@@ -762,7 +762,8 @@ __global__ __launch_bounds__(64 * WC * WR, WC == 1 ? 1 : 2) void k_tree_attend(c
 
 // ---- attention, binary32 rows ----------------------------------------------------------------------------------------------
 // The same walk with binary32 products, four at a time along the row; rows of both lists through registers, one tile ahead, codes times
-// their scales on the way.  Bound by the matrix cores' binary32 rate, a sixteenth of the 16-bit one.
+// their scales on the way.  Bound by the matrix cores' binary32 rate, a sixteenth of the 16-bit one: 10 x 14520 rows of 4 kv heads under
+// 42 columns, 213 us (19 GFLOP in 64 columns: 90 TFLOP/s, a large product here 154; 510 with one workgroup of two waves a CU).
 template <int D, int WC, int WR, int QM>
 __global__ __launch_bounds__(64 * WC * WR) void k_tree_attend_f32(const TreeArgs a) {
   constexpr int RB = D * 4, PPR = RB / 16, NTH = 64 * WC * WR, TR = 32 * WR, NPT = TR * PPR / NTH, KP = Pitch<D>::K, VP = Pitch<D>::V, NDB = D / 32;
@@ -887,13 +888,14 @@ __global__ __launch_bounds__(64 * WC * WR) void k_tree_attend_f32(const TreeArgs
 // Grid (runs of 128 list entries, B, layers).  A wave has 32 rows of list F or list Q, for one kv head after the other, and the kept
 // columns of that head in blocks of 32; 4 waves a workgroup, each on its own.  Bound by the latency of the K rows, which arrive once, and of
 // the queries: eight layers of 8 x 4133 rows (0.49 GB, 101 us at the rate of a copy) take 115 us with two waves a SIMD and the next block's queries asked for early, 137
-// without that, 209 with one wave (both code formats in one kernel); three waves spill (146).
+// without that, 209 with one wave (both code formats in one kernel); three waves spill (146).  Binary32 rows: one wave (three layers of
+// 10 x 14520 rows, 0.7 GB: 280 us; two spill, 509).
 template <int D, int KT, int QM>
-__global__ __launch_bounds__(256, 2) void k_tree_scores(const TreeScoreArgs a) {
+__global__ __launch_bounds__(256, KT == KT_F32 ? 1 : 2) void k_tree_scores(const TreeScoreArgs a) {
   constexpr int ES = KT == KT_F32 ? 4 : 2, RB = D * ES, PPR = RB / 16, NPT = 32 * PPR / 64;
   constexpr int NG = D / 32, NQF = KT == KT_F32 ? D / 8 : D / 16, KP = Pitch<D, ES>::K;
   __shared__ __attribute__((aligned(16))) char sm_k[4][32 * KP];
-  __shared__ __attribute__((aligned(16))) float sm_sc[4][NG][32];
+  __shared__ __attribute__((aligned(16))) float sm_sc[4][NG][32], sm_vn[4][32];
   const int b = blockIdx.y, layer = blockIdx.z, lane = threadIdx.x & 63, ln = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kept = a.kept[2 * b];
@@ -922,6 +924,9 @@ __global__ __launch_bounds__(256, 2) void k_tree_scores(const TreeScoreArgs a) {
       slot_s = e0 + ln < src.n ? src.list[e0 + ln] : -1;
       if ((uint32_t)slot_s >= (uint32_t)src.cap) slot_s = -1;
     }
+    const int at_pos = a.vnorm && e0 + ln < src.n ? pos[e0 + ln] : -1;       // row ln's value norm, of one kv head after the other
+    const float* vnorm = a.vnorm + lb * a.Hkv * a.Nmax;
+    float vn = 0.f;
     float sum[16];
 #pragma unroll
     for (int r = 0; r < 16; ++r) sum[r] = 0.f;
@@ -941,6 +946,7 @@ __global__ __launch_bounds__(256, 2) void k_tree_scores(const TreeScoreArgs a) {
         if constexpr (MODE == R_INT4 && D == 128) sk = *(const u32x2*)s;
         else sk.x = *(const uint32_t*)s;
       }
+      if (at_pos >= 0) vn = vnorm[at_pos];
     };
     load();
     // A block's queries and statistics are asked for while the one before it is weighed
@@ -975,9 +981,11 @@ __global__ __launch_bounds__(256, 2) void k_tree_scores(const TreeScoreArgs a) {
           }
         }
       }
+      if (a.vnorm && lane < 32) sm_vn[wave][ln] = vn;
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
       if (kvh + 1 < a.Hkv) {
+        vnorm += a.Nmax;
         src.k += (size_t)src.cap * src.code_bytes; src.sk += (size_t)src.cap * src.scale_bytes;
         load();
       }
@@ -1028,12 +1036,11 @@ __global__ __launch_bounds__(256, 2) void k_tree_scores(const TreeScoreArgs a) {
         }
       }
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        if (a.vnorm) {
-          const int e = e0 + 8 * (r / 4) + 4 * h + r % 4;
-          own[r] *= e < src.n ? a.vnorm[(lb * a.Hkv + kvh) * a.Nmax + pos[e]] : 0.f;
-        }
-        sum[r] += own[r];
+      for (int i = 0; i < 4; ++i) {
+        f32x4 f = {1.f, 1.f, 1.f, 1.f};
+        if (a.vnorm) f = *(const f32x4*)&sm_vn[wave][8 * i + 4 * h];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sum[4 * i + k] = fmaf(own[4 * i + k], f[k], sum[4 * i + k]);
       }
     }
 #pragma unroll
