@@ -359,7 +359,6 @@ __global__ __launch_bounds__(64 * WC * WR, WC == 1 ? 1 : 2) void k_tree_attend(c
   if (!run_of<TR, QM == R_INT4 ? 6 : 5>(a, r)) return;
   const int t = threadIdx.x, lane = t & 63, n = lane & 15, kb = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6), wc = wave % WC, wr = wave / WC;
-  const bool late = WC > 1 && wave >= 4;                   // (waves w and w + 4 share a SIMD)
   // Where the rows of list F's next two tiles begin, that the wave is to fetch: asked for before anything else
   const int te = r.t1 < r.tF ? r.t1 : r.tF, end = te * TR < r.nF ? te * TR : r.nF, lr = lane / PPR, lp = lane % PPR;       // the lane's row of a block, and the place of its piece
   uint32_t row[2][NBW];
@@ -421,45 +420,45 @@ __global__ __launch_bounds__(64 * WC * WR, WC == 1 ? 1 : 2) void k_tree_attend(c
 
   // ---- a tile of 32 rows in three parts.  Logits: ----
   f32x4 s[NB][2];
-  const auto logits = [&](auto mode_c, auto nb_c, const char* sm, int sc) __attribute__((always_inline)) {
-    constexpr int MODE = decltype(mode_c)::value, NC = decltype(nb_c)::value;
+  const auto logits = [&](auto mode_c, const char* sm, int sc) __attribute__((always_inline)) {
+    constexpr int MODE = decltype(mode_c)::value;
 #pragma unroll
     for (int rb = 0; rb < 2; ++rb) {
 #pragma unroll
-      for (int cb = 0; cb < NC; ++cb) s[cb][rb] = ZERO4;
+      for (int cb = 0; cb < NB; ++cb) s[cb][rb] = ZERO4;
 #pragma unroll
       for (int ks = 0; ks < NKS; ++ks) {
         const u32x4 x = *(const u32x4*)(sm + ka[ks] + rb * (BL::N / 2) * BL::KPITCH);
         if constexpr (MODE == R_INT4) {
           const f32x4 f = scales4(sc, 0, ks, rb);          // (a product is a group deep)
 #pragma unroll
-          for (int cb = 0; cb < NC; ++cb) {
+          for (int cb = 0; cb < NB; ++cb) {
             const f32x4 part = mfma_16x16x32<KT>(x, qf[cb][ks], ZERO4);
 #pragma unroll
             for (int j = 0; j < 4; ++j) s[cb][rb][j] = fmaf(f[j], part[j], s[cb][rb][j]);
           }
         } else {
 #pragma unroll
-          for (int cb = 0; cb < NC; ++cb) s[cb][rb] = mfma_16x16x32<KT>(x, qf[cb][ks], s[cb][rb]);
+          for (int cb = 0; cb < NB; ++cb) s[cb][rb] = mfma_16x16x32<KT>(x, qf[cb][ks], s[cb][rb]);
         }
       }
     }
   };
   // ---- weights, in s: of rows e0 .. ----
-  const auto weights = [&](auto mode_c, auto nb_c, int sc, int e0, int n_list) __attribute__((always_inline)) {
-    constexpr int MODE = decltype(mode_c)::value, NC = decltype(nb_c)::value;
+  const auto weights = [&](auto mode_c, int sc, int e0, int n_list) __attribute__((always_inline)) {
+    constexpr int MODE = decltype(mode_c)::value;
     if constexpr (MODE == R_INT8) {
 #pragma unroll
       for (int rb = 0; rb < 2; ++rb) {
         const f32x4 f = scales4(sc, 0, 0, rb);
 #pragma unroll
-        for (int cb = 0; cb < NC; ++cb) s[cb][rb] *= f;
+        for (int cb = 0; cb < NB; ++cb) s[cb][rb] *= f;
       }
     }
     const int tail0 = MODE == R_FULL ? r.tail0 : 0x7fffffff - 64;
     if (e0 + 32 > n_list || (MODE == R_FULL && e0 + 32 > tail0)) {      // the list's end, and the tree's rows
 #pragma unroll
-      for (int cb = 0; cb < NC; ++cb) {
+      for (int cb = 0; cb < NB; ++cb) {
         const uint32_t vis = seen_rows(sm_sees, column(cb) / a.G, e0, n_list, tail0) >> (4 * kb);
 #pragma unroll
         for (int rb = 0; rb < 2; ++rb)
@@ -467,10 +466,10 @@ __global__ __launch_bounds__(64 * WC * WR, WC == 1 ? 1 : 2) void k_tree_attend(c
           for (int j = 0; j < 4; ++j) s[cb][rb][j] = (vis >> (16 * rb + j)) & 1 ? s[cb][rb][j] : -INFINITY;
       }
     }
-    float tm[NC];                                          // the lane's own largest; the column's is looked for only if one of them calls for it
+    float tm[NB];                                          // the lane's own largest; the column's is looked for only if one of them calls for it
     bool up = false;
 #pragma unroll
-    for (int cb = 0; cb < NC; ++cb) {
+    for (int cb = 0; cb < NB; ++cb) {
       tm[cb] = s[cb][0][0];
 #pragma unroll
       for (int j = 1; j < 8; ++j) tm[cb] = fmaxf(tm[cb], s[cb][j / 4][j % 4]);
@@ -478,7 +477,7 @@ __global__ __launch_bounds__(64 * WC * WR, WC == 1 ? 1 : 2) void k_tree_attend(c
     }
     if (__builtin_amdgcn_ballot_w64(up)) {
 #pragma unroll
-      for (int cb = 0; cb < NC; ++cb) {
+      for (int cb = 0; cb < NB; ++cb) {
         const float mn = fmaxf(m[cb], max_swap16(max_swap32(tm[cb])) * a.scale2);
         scale_o(cb, mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[cb] - mn));
         m[cb] = mn;
@@ -496,7 +495,7 @@ __global__ __launch_bounds__(64 * WC * WR, WC == 1 ? 1 : 2) void k_tree_attend(c
         if (!codes) {                                      // from what rows of list F left: not so far up that it overflows
           float big = 0.f;
 #pragma unroll
-          for (int cb = 0; cb < NC; ++cb) {
+          for (int cb = 0; cb < NB; ++cb) {
             big = fmaxf(big, l[cb]);
 #pragma unroll
             for (int i = 0; i < D / 4; ++i) big = fmaxf(big, fabsf(o[cb][i / 4][i % 4]));
@@ -508,12 +507,12 @@ __global__ __launch_bounds__(64 * WC * WR, WC == 1 ? 1 : 2) void k_tree_attend(c
           codes = true;
         }
 #pragma unroll
-        for (int cb = 0; cb < NC; ++cb) scale_o(cb, ldexpf(1.f, now - oex));
+        for (int cb = 0; cb < NB; ++cb) scale_o(cb, ldexpf(1.f, now - oex));
         oex = now;
       }
     }
 #pragma unroll
-    for (int cb = 0; cb < NC; ++cb) {
+    for (int cb = 0; cb < NB; ++cb) {
       const float sub = (float)oex - (m[cb] == -INFINITY ? 0.f : m[cb]);       // (nothing seen yet: every weight is 2^-inf)
       float sum = 0.f;
 #pragma unroll
@@ -526,15 +525,15 @@ __global__ __launch_bounds__(64 * WC * WR, WC == 1 ? 1 : 2) void k_tree_attend(c
     }
   };
   // ---- and the weights, times V scales of group g, as the second product takes them ----
-  const auto terms = [&](auto mode_c, auto nb_c, auto& w, int sc, int g) __attribute__((always_inline)) {
-    constexpr int MODE = decltype(mode_c)::value, NC = decltype(nb_c)::value, N = MODE == R_FULL ? NT : NTQ;
+  const auto terms = [&](auto mode_c, auto& w, int sc, int g) __attribute__((always_inline)) {
+    constexpr int MODE = decltype(mode_c)::value, N = MODE == R_FULL ? NT : NTQ;
     f32x4 f[2];
     if constexpr (MODE != R_FULL) {
 #pragma unroll
       for (int rb = 0; rb < 2; ++rb) f[rb] = scales4(sc, 1, g, rb);
     }
 #pragma unroll
-    for (int cb = 0; cb < NC; ++cb)
+    for (int cb = 0; cb < NB; ++cb)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float p0 = s[cb][i / 2][2 * (i & 1)], p1 = s[cb][i / 2][2 * (i & 1) + 1];
@@ -545,12 +544,12 @@ __global__ __launch_bounds__(64 * WC * WR, WC == 1 ? 1 : 2) void k_tree_attend(c
         for (int k = 0; k < N; ++k) w[cb][k][i] = tw[k];
       }
   };
-  const auto outputs = [&](auto mode_c, auto nb_c, auto& w, const char* sm, int sc) __attribute__((always_inline)) {
-    constexpr int MODE = decltype(mode_c)::value, NC = decltype(nb_c)::value, N = MODE == R_FULL ? NT : NTQ;
+  const auto outputs = [&](auto mode_c, auto& w, const char* sm, int sc) __attribute__((always_inline)) {
+    constexpr int MODE = decltype(mode_c)::value, N = MODE == R_FULL ? NT : NTQ;
 #pragma unroll
     for (int db = 0; db < ND; ++db) {
       if constexpr (MODE == R_INT4) {
-        if ((db & 1) == 0) { __builtin_amdgcn_sched_barrier(0); terms(mode_c, nb_c, w, sc, db / 2); }      // (one group's at a time: registers)
+        if ((db & 1) == 0) { __builtin_amdgcn_sched_barrier(0); terms(mode_c, w, sc, db / 2); }      // (one group's at a time: registers)
       }
       union { s16x4 half[2]; u32x4 v; } x;                 // rows 4 kb + j, then 16 + 4 kb + j
 #pragma unroll
@@ -559,7 +558,7 @@ __global__ __launch_bounds__(64 * WC * WR, WC == 1 ? 1 : 2) void k_tree_attend(c
 #pragma unroll
       for (int k = 0; k < N; ++k)
 #pragma unroll
-        for (int cb = 0; cb < NC; ++cb) o[cb][db] = mfma_16x16x32<(MODE == R_FULL ? KT : KT_F16)>(x.v, w[cb][k], o[cb][db]);
+        for (int cb = 0; cb < NB; ++cb) o[cb][db] = mfma_16x16x32<(MODE == R_FULL ? KT : KT_F16)>(x.v, w[cb][k], o[cb][db]);
     }
   };
   // A list's tiles from t0 to t1 (32 rows of every row wave each), with a barrier a tile; fetch brings the next one into the other stage.
@@ -570,11 +569,10 @@ __global__ __launch_bounds__(64 * WC * WR, WC == 1 ? 1 : 2) void k_tree_attend(c
       fetch(ic, tile);
       if (c0 < c1) {
         u32x4 w[NB][MODE == R_FULL ? NT : NTQ];
-        constexpr std::integral_constant<int, NB> nb_c{};
-        logits(mode_c, nb_c, i ? sm_k1 : sm_k0, i);
-        weights(mode_c, nb_c, i, tile * TR + 32 * wr, n_list);
-        if constexpr (MODE != R_INT4) terms(mode_c, nb_c, w, i, 0);
-        outputs(mode_c, nb_c, w, i ? sm_v1 : sm_v0, i);
+        logits(mode_c, i ? sm_k1 : sm_k0, i);
+        weights(mode_c, i, tile * TR + 32 * wr, n_list);
+        if constexpr (MODE != R_INT4) terms(mode_c, w, i, 0);
+        outputs(mode_c, w, i ? sm_v1 : sm_v0, i);
       }
       if constexpr (MODE == R_FULL) wait_rows<0, (WC > 1)>();
       else lds_barrier<(WC > 1)>();
